@@ -605,6 +605,198 @@ topkv_status_t topkv_reblock_layer(const topkv_pool_t* src, int32_t src_layer, c
                                    const int32_t* dst_tables, int32_t dst_stride, int32_t num_reqs,
                                    const int32_t* seq_lens, hipStream_t stream);
 
+/* ---- Attention over a paged cache ---------------------------------------------
+ * What a worker does with the pages once it holds them (Section 6: paged pools
+ * reached through block tables; Section 5.3: one latent shared by all heads).
+ *
+ * The cache is a pool view (TOPKV_LAYOUT_POOL or TOPKV_LAYOUT_POOL_HEAD_MAJOR):
+ * its layer, block tables (device int32[num_reqs][bt_stride]) and head_begin,
+ * the first of the kv_heads KV heads that the query heads share; `shards` is
+ * ignored.  Query head h uses KV head head_begin + h / (num_heads / kv_heads).
+ * With planes = 2 plane 0 holds keys and plane 1 values of head_dim elements;
+ * with planes = 1 (a latent cache) the key is the whole row and the value its
+ * first value_dim elements.
+ *
+ * For the token at position p of a request of n tokens (its own key and value
+ * already lie in the cache), with V the positions j <= p that it sees,
+ *     window == 0: every j;  window > 0: j > p - window or j < sinks,
+ * less those whose page lies outside [0, num_pages):
+ *     x_j = scale * k_scale * (q . k_j)
+ *     out = v_scale * sum_V exp(x_j) v_j / sum_V exp(x_j)
+ *     lse = ln sum_V exp(x_j)
+ * and out = 0, lse = -inf where V is empty (a request of no tokens among
+ * them) or every x_j in it is -inf.  What a cache holds outside V never reaches a row's result, NaN and
+ * infinities included.  Sums and softmax statistics are 32-bit floats. */
+typedef enum topkv_dtype {
+  TOPKV_BF16 = 0,
+  TOPKV_FP16 = 1,
+  TOPKV_FP8_E4M3 = 2    /* caches only: OCP e4m3 (no infinities), value = element * k_scale or v_scale */
+} topkv_dtype_t;
+
+typedef struct topkv_attention {
+  int32_t dtype;       /* of q and out: TOPKV_BF16 or TOPKV_FP16 */
+  int32_t kv_dtype;    /* of the cache: `dtype` or TOPKV_FP8_E4M3 */
+  int32_t num_heads;   /* query heads, a multiple of kv_heads */
+  int32_t kv_heads;    /* KV heads read, from the view's head_begin */
+  int32_t value_dim;   /* planes 2: head_dim; planes 1: 1 .. head_dim */
+  int32_t window;      /* 0: every earlier token is seen */
+  int32_t sinks;       /* with a window: first tokens of the request that stay visible, >= 0 */
+  int32_t reserved;    /* set to 0 */
+  float   scale;       /* > 0, finite (usually head_dim^-1/2) */
+  float   k_scale;     /* > 0, finite (1 for 16-bit caches) */
+  float   v_scale;     /* finite */
+  float   reserved2;   /* set to 0 */
+  int64_t q_stride;    /* elements between tokens of q, >= num_heads * head_dim */
+  int64_t out_stride;  /* elements between tokens of out, >= num_heads * value_dim */
+} topkv_attention_t;
+
+/* Bytes of device memory the two calls below need as workspace for up to
+ * num_reqs requests and total_q query tokens (decode: num_reqs); -1 for a bad
+ * view, options or counts.  Depends on the geometry, not on device contents.
+ * Contents are scratch: nothing in it outlives a call, and it needs no
+ * initial values.  Calls that may overlap in time (other streams, graphs that
+ * run side by side) each need one of their own. */
+int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_attention_t* attn,
+                                        int32_t num_reqs, int32_t total_q);
+
+/* One new token per request: request r's query is row r of q
+ * ([num_reqs][num_heads][head_dim]) and sits at position seq_lens[r] - 1.
+ *   seq_lens:  device int32[num_reqs], the new token counted; clamped to
+ *              [0, bt_stride * page_size]
+ *   q, out:    device, out [num_reqs][num_heads][value_dim]; must not overlap
+ *   lse:       device float[num_reqs][num_heads], or NULL
+ *   workspace: device memory, 16-byte aligned (may be NULL when
+ *              topkv_attention_workspace_bytes is 0)
+ * num_reqs == 0 launches nothing.  Any head_dim up to 1024; rows of q, out
+ * and the cache that are multiples of 16 bytes (8 for an 8-bit cache) on such
+ * addresses with head_dim up to 256 (planes 1: up to 576) run on the matrix
+ * units, others on a slower general kernel.  Errors: TOPKV_ERR_INVALID_ARG for bad
+ * descriptors, options, null pointers or a short or misaligned workspace,
+ * TOPKV_ERR_UNSUPPORTED for head_dim above 1024, more than
+ * TOPKV_MAX_BATCH_REQS requests, bt_stride * page_size of 2^31 or more or
+ * 2^31 (token, head) rows, TOPKV_ERR_LAUNCH.  Does not synchronise and can be
+ * captured into a graph. */
+topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_attention_t* attn,
+                                      int32_t num_reqs, const int32_t* seq_lens, const void* q, void* out,
+                                      float* lse, void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* Any number of new tokens per request (a prompt, a chunk of one, or the few
+ * tokens of a draft): request r's are rows q_starts[r] .. q_starts[r + 1] - 1
+ * of q, the last of them at position seq_lens[r] - 1.
+ *   q_starts:  device int32[num_reqs + 1], ascending; clamped to [0, total_q]
+ *   total_q:   rows of q, out and lse; rows that belong to no request are
+ *              left as they were
+ * A token whose position would be negative (more new tokens than seq_lens[r])
+ * sees nothing.  Otherwise as topkv_attention_decode; total_q == 0 launches
+ * nothing. */
+topkv_status_t topkv_attention_prompt(const topkv_view_t* cache, const topkv_attention_t* attn,
+                                      int32_t num_reqs, const int32_t* seq_lens, const int32_t* q_starts,
+                                      int32_t total_q, const void* q, void* out, float* lse, void* workspace,
+                                      int64_t workspace_bytes, hipStream_t stream);
+
+/* ---- Pages: sharing, taking, giving back, compacting, copying ------------------
+ * Who holds which page of a pool, on the device.  A row is one request's line
+ * of the block tables; it holds the pages of its first
+ * ceil(seq_lens[row] / page_size) entries.  ref_counts[p] is the number of
+ * held entries, over all rows, that name page p; a page with count 0 is free.
+ * A free page is taken lowest index first, so results depend on the state
+ * alone.  The tables are those that pack, unpack and attention read. */
+typedef struct topkv_page_owner {
+  int32_t* ref_counts;    /* device int32[num_pages] */
+  int32_t* block_tables;  /* device int32[num_rows][bt_stride] */
+  int32_t* seq_lens;      /* device int32[num_rows] */
+  int64_t  num_pages;     /* > 0, below 2^31 */
+  int32_t  page_size;     /* > 0 */
+  int32_t  num_rows;      /* > 0 */
+  int32_t  bt_stride;     /* > 0; bt_stride * page_size below 2^31 */
+  int32_t  reserved;      /* set to 0 */
+} topkv_page_owner_t;
+
+/* Every call below writes result, device int32[4], on the stream:
+ *   [0] TOPKV_OK or TOPKV_ERR_BOUNDS
+ *   [1] pairs written (0 where a call writes none or did nothing)
+ *   [2] pages: counted, given back, taken (or, when too few are free, how
+ *       many were wanted), or live
+ *   [3] bad rows (count, free and compact: bad entries too)
+ * A (source page, destination page) pair means that the caller has to copy
+ * that page in every layer (topkv_copy_pages) before the next call that takes
+ * pages, and before the destination is read or written.  result + 1 serves as
+ * topkv_copy_pages' count.  None of the calls allocates or synchronises; all
+ * can be captured.  Calls on one owner have to be ordered (one stream).
+ * TOPKV_ERR_INVALID_ARG for a bad descriptor, null pointers, a negative or
+ * (above num_rows or TOPKV_MAX_BATCH_REQS) too large number of rows, too few
+ * pairs or a short or misaligned workspace. */
+
+/* Workspace bytes of fork, grow and compact for this owner (16-byte aligned
+ * device memory, scratch); -1 for a bad descriptor. */
+int64_t topkv_pages_workspace_bytes(const topkv_page_owner_t* owner);
+
+/* ref_counts from the tables: for tables that were filled elsewhere.  Entries
+ * outside the pool are left out and make result[0] TOPKV_ERR_BOUNDS, as do
+ * lengths outside [0, bt_stride * page_size] (that row is left out). */
+topkv_status_t topkv_pages_count(const topkv_page_owner_t* owner, int32_t* result, hipStream_t stream);
+
+/* Rows rows[0 .. num) keep their first keep_lens[i] tokens (keep_lens NULL:
+ * none) and give back the pages past them: those entries become -1, their
+ * counts fall by one, seq_lens[row] becomes min(seq_lens[row], keep).  A row
+ * named twice ends at the smaller length.  Rows outside [0, num_rows), bad
+ * lengths, entries outside the pool and entries whose count is 0 already are
+ * skipped and counted in result[3] (result[0] TOPKV_ERR_BOUNDS). */
+topkv_status_t topkv_pages_free(const topkv_page_owner_t* owner, int32_t num, const int32_t* rows,
+                                const int32_t* keep_lens, int32_t* result, hipStream_t stream);
+
+/* Row children[i] branches off row parents[i]: it gets the parent's length,
+ * shares its full pages and, where the last page is partial, takes a page of
+ * its own for it and writes the pair, in order of i.  A parent may occur many
+ * times; children must be distinct and hold nothing (seq_lens 0).  Where a
+ * row is bad (out of range, not empty, named twice, a parent of bad length)
+ * or too few pages are free, nothing changes and result[0] is
+ * TOPKV_ERR_BOUNDS.  A parent's entry outside the pool goes to the child as
+ * it is, counted in result[3] (result[0] TOPKV_ERR_BOUNDS; the rest is done).
+ *   pairs: device int32[max_pairs][2], max_pairs >= num */
+topkv_status_t topkv_pages_fork(const topkv_page_owner_t* owner, int32_t num, const int32_t* parents,
+                                const int32_t* children, int32_t* pairs, int32_t max_pairs, void* workspace,
+                                int64_t workspace_bytes, int32_t* result, hipStream_t stream);
+
+/* Rows rows[0 .. num) take the pages for new_lens[i] tokens, in order of i.
+ * A partial last page that other rows share (it would be written) is replaced
+ * by a page of the row's own: the pair is written and the shared page's count
+ * falls by one.  Rows must be distinct, new_lens[i] in [seq_lens[row],
+ * bt_stride * page_size]; otherwise, or with too few free pages, nothing
+ * changes and result[0] is TOPKV_ERR_BOUNDS.
+ *   pairs: device int32[max_pairs][2], max_pairs >= num */
+topkv_status_t topkv_pages_grow(const topkv_page_owner_t* owner, int32_t num, const int32_t* rows,
+                                const int32_t* new_lens, int32_t* pairs, int32_t max_pairs, void* workspace,
+                                int64_t workspace_bytes, int32_t* result, hipStream_t stream);
+
+/* Moves the live pages together: with U live pages, the highest one goes to
+ * the lowest free page, and so on until pages 0 .. U - 1 are the live ones.
+ * ref_counts and the held entries of every row follow; result[2] = U, and the
+ * pairs (at most num_pages / 2) say what to copy.  Held entries outside the
+ * pool and rows of bad length stay as they are and are counted in result[3]
+ * (result[0] TOPKV_ERR_BOUNDS; the rest is moved).  ref_counts have to agree
+ * with the tables (topkv_pages_count): an entry that names a free page may
+ * name another row's page afterwards.
+ *   pairs: device int32[max_pairs][2], max_pairs >= num_pages / 2 */
+topkv_status_t topkv_pages_compact(const topkv_page_owner_t* owner, int32_t* pairs, int32_t max_pairs,
+                                   void* workspace, int64_t workspace_bytes, int32_t* result,
+                                   hipStream_t stream);
+
+/* Copies whole pages: for each pair (s, d) and each layer l of [first_layer,
+ * first_layer + num_layers), page s of layer l of `src` to page d of layer l
+ * of `dst`.  The pools agree on planes, page_size, num_heads, head_dim and
+ * elem_bytes and may be one and the same; no page may be a destination and
+ * named again.  Pairs with a page outside its pool are skipped.
+ *   pairs:     device int32[max_pairs][2]
+ *   count:     device int32 holding how many of them to copy (clamped to
+ *              [0, max_pairs]), or NULL for all
+ * TOPKV_ERR_INVALID_ARG for bad or different geometries, a layer range
+ * outside a pool, null pairs or a negative max_pairs; max_pairs == 0 or
+ * num_layers == 0 launches nothing.  One kernel; does not synchronise. */
+topkv_status_t topkv_copy_pages(const topkv_pool_t* src, const topkv_pool_t* dst, int32_t first_layer,
+                                int32_t num_layers, const int32_t* pairs, int32_t max_pairs,
+                                const int32_t* count, hipStream_t stream);
+
 /* ---- Fixed-state layers (Section 2.2) ------------------------------------
  * Section 2.2 extends Eq. 1 per layer kind: a linear-attention layer holds,
  * per request, a state whose size does not depend on the sequence length.

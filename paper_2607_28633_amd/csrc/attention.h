@@ -1,0 +1,82 @@
+// attention.h - what the attention kernels share (attention.hip: the calls and
+// the general kernel; attention_decode.hip, attention_prompt.hip: the matrix-unit kernels).
+#ifndef TOPKV_ATTENTION_H_
+#define TOPKV_ATTENTION_H_
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "topkv.h"
+
+namespace topkv_attend {
+
+// One call, validated.  Byte strides of the cache; element strides of q and out.
+struct Args {
+  const char* cache;          // layer and first KV head
+  const int32_t* tables;      // [num_reqs][bt_stride]
+  const int32_t* seq_lens;    // [num_reqs]
+  const int32_t* q_starts;    // [num_reqs + 1], or null: one token per request
+  const void* q;
+  void* out;
+  float* lse;                 // may be null
+  int64_t num_pages;
+  int64_t page_bytes, slot_bytes, head_bytes;
+  int64_t value_bytes;        // from a key row to its value row
+  int64_t q_stride, out_stride;
+  int32_t page_size, bt_stride, num_reqs, total_q;
+  int32_t num_heads, kv_heads, group;
+  int32_t head_dim, value_dim;
+  int32_t window, sinks;
+  float scale;                // scale * k_scale * log2(e): scores in powers of two
+  float v_scale;
+  int32_t dtype, kv_dtype;
+};
+
+constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ int32_t clamped_len(const Args& a, int32_t r) {
+  const int32_t n = a.seq_lens[r], cap = a.bt_stride * a.page_size;
+  return n < 0 ? 0 : n > cap ? cap : n;
+}
+
+__device__ __forceinline__ int32_t clamped_start(const Args& a, int32_t r) {
+  const int32_t s = a.q_starts[r];
+  return s < 0 ? 0 : s > a.total_q ? a.total_q : s;
+}
+
+// The keys that positions [first, last] of a request see lie at positions
+// [0, head) and [start, last + 1): numbered 0 .. head + last + 1 - start in
+// that order.  Without a window head = start = 0.
+struct Span {
+  int32_t head, start, count;
+};
+
+__device__ __forceinline__ Span key_span(const Args& a, int32_t first, int32_t last) {
+  Span s;
+  const int32_t from = first < 0 ? 0 : first;
+  s.start = (a.window > 0 && from >= a.window) ? from - a.window + 1 : 0;
+  s.head = a.sinks < s.start ? a.sinks : s.start;
+  s.count = last < 0 ? 0 : s.head + last + 1 - s.start;
+  return s;
+}
+
+__device__ __forceinline__ int32_t key_position(const Span& s, int32_t i) { return i < s.head ? i : i - s.head + s.start; }
+
+__device__ __forceinline__ bool sees(const Args& a, int32_t pos, int32_t j) {
+  return j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
+}
+
+// Byte offset of position j's row from a.cache, or -1 when its page lies
+// outside the pool.
+__device__ __forceinline__ int64_t row_offset(const Args& a, const int32_t* __restrict__ table, int32_t j) {
+  const uint32_t page = (uint32_t)j / (uint32_t)a.page_size;
+  const int32_t e = table[page];
+  if (e < 0 || e >= a.num_pages) return -1;
+  return (int64_t)e * a.page_bytes + (int64_t)((uint32_t)j - page * (uint32_t)a.page_size) * a.slot_bytes;
+}
+
+}  // namespace topkv_attend
+
+#endif  // TOPKV_ATTENTION_H_

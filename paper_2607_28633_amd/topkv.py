@@ -51,11 +51,19 @@ EXPORTS = ["topkv_pack_layer", "topkv_unpack_layer", "topkv_pack_layer_batched",
            "topkv_pack_state_layer", "topkv_unpack_state_layer", "topkv_check_state_slots",
            "topkv_check_state_workspace_bytes", "topkv_kvcache1_pack_layers", "topkv_kvcache1_unpack_layers",
            "topkv_kvcache1_pack_seal", "topkv_kvcache1_verify_unpack", "topkv_engine_pack_layers",
-           "topkv_engine_unpack_layers", "topkv_engine_layers_per_grid", "topkv_crc64_noalloc"]
+           "topkv_engine_unpack_layers", "topkv_engine_layers_per_grid", "topkv_crc64_noalloc",
+           "topkv_attention_workspace_bytes", "topkv_attention_decode", "topkv_attention_prompt",
+           "topkv_pages_workspace_bytes", "topkv_pages_count", "topkv_pages_free", "topkv_pages_fork",
+           "topkv_pages_grow", "topkv_pages_compact", "topkv_copy_pages"]
 
 TOPKV_LAYOUT_PACKED = 0
 TOPKV_LAYOUT_POOL = 1
 TOPKV_LAYOUT_POOL_HEAD_MAJOR = 2
+
+TOPKV_BF16 = 0
+TOPKV_FP16 = 1
+TOPKV_FP8_E4M3 = 2
+_DTYPE = {torch.bfloat16: TOPKV_BF16, torch.float16: TOPKV_FP16, torch.float8_e4m3fn: TOPKV_FP8_E4M3}
 
 
 class topkv_pool_t(ctypes.Structure):
@@ -77,6 +85,20 @@ class topkv_state_pool_t(ctypes.Structure):
                 ("num_layers", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class topkv_attention_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32), ("num_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("value_dim", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("reserved", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("reserved2", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+class topkv_page_owner_t(ctypes.Structure):
+    _fields_ = [("ref_counts", ctypes.c_void_p), ("block_tables", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("num_rows", ctypes.c_int32),
+                ("bt_stride", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class topkv_launch_t(ctypes.Structure):
     _fields_ = [("stream", ctypes.c_void_p), ("start", ctypes.c_void_p), ("stop", ctypes.c_void_p)]
 
@@ -91,6 +113,9 @@ _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _POOL = ctypes.POINTER(topkv_pool_t)
+_VIEW = ctypes.POINTER(topkv_view_t)
+_ATTN = ctypes.POINTER(topkv_attention_t)
+_OWNER = ctypes.POINTER(topkv_page_owner_t)
 _SIGS = {
     "topkv_pack_layer": (_I32, [_POOL, _I32, _P, _I32, _P, _P]),
     "topkv_unpack_layer": (_I32, [_P, _POOL, _I32, _P, _I32, _P]),
@@ -150,6 +175,16 @@ _SIGS = {
     "topkv_dma_submit": (_I32, [_P, _P, _P, _P, _I64, ctypes.POINTER(_I64)]),
     "topkv_dma_wait": (_I32, [_P, _I64]),
     "topkv_dma_destroy": (_I32, [_P]),
+    "topkv_attention_workspace_bytes": (_I64, [_VIEW, _ATTN, _I32, _I32]),
+    "topkv_attention_decode": (_I32, [_VIEW, _ATTN, _I32, _P, _P, _P, _P, _P, _I64, _P]),
+    "topkv_attention_prompt": (_I32, [_VIEW, _ATTN, _I32, _P, _P, _I32, _P, _P, _P, _P, _I64, _P]),
+    "topkv_pages_workspace_bytes": (_I64, [_OWNER]),
+    "topkv_pages_count": (_I32, [_OWNER, _P, _P]),
+    "topkv_pages_free": (_I32, [_OWNER, _I32, _P, _P, _P, _P]),
+    "topkv_pages_fork": (_I32, [_OWNER, _I32, _P, _P, _P, _I32, _P, _I64, _P, _P]),
+    "topkv_pages_grow": (_I32, [_OWNER, _I32, _P, _P, _P, _I32, _P, _I64, _P, _P]),
+    "topkv_pages_compact": (_I32, [_OWNER, _P, _I32, _P, _I64, _P, _P]),
+    "topkv_copy_pages": (_I32, [_POOL, _POOL, _I32, _I32, _P, _I32, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -810,3 +845,159 @@ def topkv_check_state_slots(pool, num_reqs, slots, result, check_duplicates=True
     _check(_lib.topkv_check_state_slots(ctypes.byref(_state_arg(pool)), int(num_reqs), _table_ptr(slots),
                                         int(bool(check_duplicates)), _ptr(workspace), wsb, _ptr(result),
                                         _stream(stream)))
+
+
+# --- attention over a paged cache -------------------------------------------------
+
+def _token_stride(t: torch.Tensor) -> int:
+    """Elements between tokens of a [tokens][heads][dim] tensor whose heads lie side by side."""
+    if t.dim() != 3:
+        raise ValueError("expected a [tokens][heads][dim] tensor")
+    T, H, D = t.shape
+    if t.numel() and ((D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D)):
+        raise ValueError("a token's heads must be contiguous (any stride between tokens)")
+    return max(int(t.stride(0)), H * D) if T > 1 else H * D
+
+
+def _rows_ptr(x) -> int:
+    """Device address of a [tokens][heads][dim] tensor with any stride between tokens (or an address)."""
+    if isinstance(x, torch.Tensor):
+        if not x.is_cuda and x.numel():
+            raise ValueError("tensor arguments must live in device memory")
+        if x.dim() == 3:
+            if x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2]:
+                raise ValueError("tokens must not overlap")
+            _token_stride(x)
+            return x.data_ptr()
+    return _ptr(x)
+
+
+def attention_options(q, out, *, kv_heads, scale, kv_dtype=None, window=0, sinks=0, k_scale=1.0,
+                      v_scale=1.0) -> topkv_attention_t:
+    """Options of the attention calls for query and output tensors
+    [tokens][heads][dim] / [tokens][heads][value_dim] (bfloat16 or float16, any
+    stride between tokens).  kv_dtype: the cache's element type (default: q's)."""
+    if q.dtype != out.dtype or q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q and out must be both bfloat16 or both float16")
+    if q.dim() != 3 or out.dim() != 3 or q.shape[:2] != out.shape[:2]:
+        raise ValueError("q and out must be [tokens][heads][dim] with the same tokens and heads")
+    kv = _DTYPE.get(q.dtype if kv_dtype is None else kv_dtype)
+    if kv is None:
+        raise ValueError("the cache must be of q's type or float8_e4m3fn")
+    return topkv_attention_t(_DTYPE[q.dtype], kv, q.shape[1], int(kv_heads), out.shape[2], int(window), int(sinks), 0,
+                             float(scale), float(k_scale), float(v_scale), 0.0, _token_stride(q), _token_stride(out))
+
+
+def _lse_ptr(t) -> int:
+    if isinstance(t, torch.Tensor) and t.dtype != torch.float32:
+        raise ValueError("lse must be float32")
+    return _ptr(t)
+
+
+def topkv_attention_workspace_bytes(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, total_q) -> int:
+    n = _lib.topkv_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(attn), int(num_reqs), int(total_q))
+    if n < 0:
+        raise TopkvError(TOPKV_ERR_INVALID_ARG)
+    return n
+
+
+def prepare_attention_decode(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q, out, workspace=None,
+                             lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
+    wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
+    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)), _P(_rows_ptr(q)),
+            _P(_rows_ptr(out)), _P(_lse_ptr(lse)), _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
+    return PreparedCall("topkv_attention_decode", args, (cache, attn))
+
+
+def prepare_attention_prompt(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q_starts, total_q, q, out,
+                             workspace=None, lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
+    wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
+    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)),
+            _P(_table_ptr(q_starts)), _I32(int(total_q)), _P(_rows_ptr(q)), _P(_rows_ptr(out)), _P(_lse_ptr(lse)),
+            _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
+    return PreparedCall("topkv_attention_prompt", args, (cache, attn))
+
+
+def topkv_attention_decode(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q, out, workspace=None,
+                           lse=None, workspace_bytes=None, stream=None) -> None:
+    """One new token per request: row r of q attends to request r's cache."""
+    prepare_attention_decode(cache, attn, num_reqs, seq_lens, q, out, workspace, lse, workspace_bytes, stream)()
+
+
+def topkv_attention_prompt(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q_starts, total_q, q, out,
+                           workspace=None, lse=None, workspace_bytes=None, stream=None) -> None:
+    """New tokens q_starts[r] .. q_starts[r + 1] - 1 of q attend to request r's cache, each to what precedes it."""
+    prepare_attention_prompt(cache, attn, num_reqs, seq_lens, q_starts, total_q, q, out, workspace, lse, workspace_bytes,
+                             stream)()
+
+
+# --- pages: sharing, taking, giving back, compacting, copying -------------------------
+
+def page_owner(ref_counts, block_tables, seq_lens, *, page_size, num_pages=None, num_rows=None,
+               bt_stride=None) -> topkv_page_owner_t:
+    """Descriptor of who holds which page: int32 tensors ref_counts [pages],
+    block_tables [rows][stride] and seq_lens [rows] (or addresses with the sizes given)."""
+    if num_pages is None:
+        num_pages = ref_counts.numel()
+    if num_rows is None or bt_stride is None:
+        num_rows, bt_stride = block_tables.shape
+    return topkv_page_owner_t(_table_ptr(ref_counts), _table_ptr(block_tables), _table_ptr(seq_lens), int(num_pages),
+                              int(page_size), int(num_rows), int(bt_stride), 0)
+
+
+def _pairs(t, given):
+    if given is None:
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("the number of pairs is required when passing a raw address")
+        given = t.numel() // 2
+    return _P(_table_ptr(t)), _I32(int(given))
+
+
+def topkv_pages_workspace_bytes(owner: topkv_page_owner_t) -> int:
+    n = _lib.topkv_pages_workspace_bytes(ctypes.byref(owner))
+    if n < 0:
+        raise TopkvError(TOPKV_ERR_INVALID_ARG)
+    return n
+
+
+def topkv_pages_count(owner: topkv_page_owner_t, result, stream=None) -> None:
+    """ref_counts from the tables; result (device int32[4], for every call
+    here): [status, pairs, pages, bad rows or entries]."""
+    _check(_lib.topkv_pages_count(ctypes.byref(owner), _table_ptr(result), _stream(stream)))
+
+
+def topkv_pages_free(owner: topkv_page_owner_t, num, rows, result, keep_lens=None, stream=None) -> None:
+    """Rows give back the pages past their first keep_lens[i] tokens (None: all)."""
+    _check(_lib.topkv_pages_free(ctypes.byref(owner), int(num), _table_ptr(rows), _table_ptr(keep_lens),
+                                 _table_ptr(result), _stream(stream)))
+
+
+def topkv_pages_fork(owner: topkv_page_owner_t, num, parents, children, pairs, workspace, result, max_pairs=None,
+                     workspace_bytes=None, stream=None) -> None:
+    """Rows children[i] branch off rows parents[i]."""
+    _check(_lib.topkv_pages_fork(ctypes.byref(owner), int(num), _table_ptr(parents), _table_ptr(children),
+                                 *_pairs(pairs, max_pairs), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                 _table_ptr(result), _stream(stream)))
+
+
+def topkv_pages_grow(owner: topkv_page_owner_t, num, rows, new_lens, pairs, workspace, result, max_pairs=None,
+                     workspace_bytes=None, stream=None) -> None:
+    """Rows take the pages for new_lens[i] tokens."""
+    _check(_lib.topkv_pages_grow(ctypes.byref(owner), int(num), _table_ptr(rows), _table_ptr(new_lens),
+                                 *_pairs(pairs, max_pairs), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                 _table_ptr(result), _stream(stream)))
+
+
+def topkv_pages_compact(owner: topkv_page_owner_t, pairs, workspace, result, max_pairs=None, workspace_bytes=None,
+                        stream=None) -> None:
+    """Move the live pages together at the pool's lower end."""
+    _check(_lib.topkv_pages_compact(ctypes.byref(owner), *_pairs(pairs, max_pairs), _ptr(workspace),
+                                    _nbytes(workspace, workspace_bytes), _table_ptr(result), _stream(stream)))
+
+
+def topkv_copy_pages(src, dst, first_layer, num_layers, pairs, max_pairs=None, count=None, stream=None) -> None:
+    """Copy whole pages by (source, destination) pairs in a range of layers;
+    count: a device int32 (tensor or address), or None for all pairs."""
+    ptr, most = _pairs(pairs, max_pairs)
+    _check(_lib.topkv_copy_pages(ctypes.byref(_pool_arg(src)), ctypes.byref(_pool_arg(dst)), int(first_layer),
+                                 int(num_layers), ptr, most, _table_ptr(count), _stream(stream)))
