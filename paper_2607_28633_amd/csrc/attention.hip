@@ -5,6 +5,7 @@
 
 #include <cmath>
 
+#include "attention_internal.h"
 #include "internal.h"
 
 namespace topkv_attend {
@@ -155,7 +156,7 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
   if (t->q_stride < (int64_t)t->num_heads * p.head_dim || t->out_stride < (int64_t)t->num_heads * t->value_dim)
     return TOPKV_ERR_INVALID_ARG;
   if (num_reqs < 0 || total_q < 0) return TOPKV_ERR_INVALID_ARG;
-  if (p.head_dim > 1024 || num_reqs > TOPKV_MAX_BATCH_REQS || (int64_t)v->bt_stride * p.page_size > INT32_MAX ||
+  if (p.head_dim > 1024 || num_reqs > TOPKV_MAX_BATCH_REQS || (int64_t)v->bt_stride * p.page_size >= (1 << 30) ||
       (int64_t)total_q * t->num_heads > INT32_MAX)
     return TOPKV_ERR_UNSUPPORTED;
   const int64_t elem = p.elem_bytes, plane = (int64_t)p.page_size * p.num_heads * p.head_dim * elem;
@@ -188,6 +189,13 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
   return TOPKV_OK;
 }
 
+// Rows of q and the cache on 16-byte addresses (8 for an 8-bit cache).
+bool aligned(const Args& a) {
+  const uintptr_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
+  return reinterpret_cast<uintptr_t>(a.cache) % unit == 0 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 &&
+         a.q_stride % 8 == 0;
+}
+
 topkv_status_t attend(const topkv_view_t* cache, const topkv_attention_t* attn, int32_t num_reqs, const int32_t* seq_lens,
                       const int32_t* q_starts, bool decode, int32_t total_q, const void* q, void* out, float* lse,
                       void* workspace, int64_t workspace_bytes, hipStream_t stream) {
@@ -206,6 +214,7 @@ topkv_status_t attend(const topkv_view_t* cache, const topkv_attention_t* attn, 
   a.q = q;
   a.out = out;
   a.lse = lse;
+  if (decode && decode_takes(a) && aligned(a)) return run_decode(a, workspace, stream);
   return run_general(a, stream);
 }
 
@@ -217,7 +226,7 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
                                         int32_t total_q) {
   topkv_attend::Args a;
   if (topkv_attend::describe(cache, attn, num_reqs, total_q, &a) != TOPKV_OK) return -1;
-  return 0;
+  return topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a) : 0;
 }
 
 topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_attention_t* attn, int32_t num_reqs,

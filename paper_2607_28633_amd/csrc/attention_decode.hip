@@ -1,0 +1,438 @@
+// attention_decode.hip - one new token per request on the matrix units.
+//
+// A request's group of query heads (up to 16 rows) reads each key and value
+// once: 2 * group flops per cache element, so the kernel is bound by the
+// cache's bytes.  A wave keeps the rows in registers and walks tiles of 32
+// keys: the next tile is on its way to registers while the present one, in
+// the wave's own piece of LDS, is multiplied; no barrier is needed on the way.
+// The four waves of a workgroup take tiles in turn and join at the end.
+//
+// Few requests would leave most of the GPU idle, uneven ones would wait for
+// the longest: the visible tokens of the whole batch are cut into chunks of
+// one size, as many as keep the GPU busy, and requests of several chunks are
+// joined by a second kernel from partial results in 32 bits.  The cut follows
+// the lengths on the device, not the width of the tables.
+#include "attention_internal.h"
+#include "attention_mfma.h"
+
+namespace topkv_attend {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kTile = 32;                // keys of one wave's tile
+constexpr int kRows = 16;                // query rows of a workgroup
+constexpr int kStep = kTile * kWaves;    // keys of the workgroup's tiles
+
+struct Plan {
+  int32_t chunks;      // wanted over all requests; 0: one per request, whatever its length
+  int32_t slots;       // partial results that fit (requests of one chunk need none)
+  float* part;         // [slot][kv head][row of the group][value_dim]
+  float2v* part_ml;    // [slot][kv head][row of the group]: maximum and sum
+  int2* cut;           // [request]: chunks, first slot
+};
+
+struct Item {
+  int32_t request, chunk, of, slot;      // slot: of the request's first chunk
+};
+
+__device__ __forceinline__ int32_t decode_count(const Args& a, int32_t r) {
+  const int32_t p = clamped_len(a, r) - 1;
+  return key_span(a, p, p).count;
+}
+
+// Which request and chunk item number `item` is; false past the last.
+__device__ bool find_item(const Args& a, const Plan& p, int32_t item, Item* got) {
+  __shared__ int64_t s_total[kWaves];
+  __shared__ int32_t s_items[kWaves], s_slots[kWaves];
+  __shared__ Item s_got;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t per = (a.num_reqs + kThreads - 1) / kThreads;
+  const int32_t lo = threadIdx.x * per, hi = lo + per < a.num_reqs ? lo + per : a.num_reqs;
+  int64_t total = 0;
+  for (int32_t r = lo; r < hi; ++r) total += decode_count(a, r);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
+  if (lane == 0) s_total[wave] = total;
+  if (threadIdx.x == 0) s_got.request = -1;
+  __syncthreads();
+  total = 0;
+  for (int i = 0; i < kWaves; ++i) total += s_total[i];
+  int64_t size = (total + p.chunks - 1) / p.chunks;
+  size = size < 2 * kStep ? 2 * kStep : (size + kStep - 1) / kStep * kStep;
+  int32_t items = 0, slots = 0;
+  for (int32_t r = lo; r < hi; ++r) {
+    const int32_t n = (int32_t)((decode_count(a, r) + size - 1) / size), c = n < 1 ? 1 : n;
+    items += c;
+    slots += c > 1 ? c : 0;
+  }
+  int32_t items_inc = items, slots_inc = slots;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t x = __shfl_up(items_inc, d, 64), y = __shfl_up(slots_inc, d, 64);
+    if (lane >= d) items_inc += x, slots_inc += y;
+  }
+  if (lane == 63) s_items[wave] = items_inc, s_slots[wave] = slots_inc;
+  __syncthreads();
+  int32_t at = items_inc - items, slot = slots_inc - slots;
+  for (int i = 0; i < wave; ++i) at += s_items[i], slot += s_slots[i];
+  if (item >= at && item < at + items) {
+    for (int32_t r = lo; r < hi; ++r) {
+      const int32_t n = (int32_t)((decode_count(a, r) + size - 1) / size), c = n < 1 ? 1 : n;
+      if (item < at + c) {
+        s_got.request = r;
+        s_got.chunk = item - at;
+        s_got.of = c;
+        s_got.slot = slot;
+        break;
+      }
+      at += c;
+      slot += c > 1 ? c : 0;
+    }
+  }
+  __syncthreads();
+  *got = s_got;
+  return got->request >= 0;
+}
+
+// KD, VD: key and value elements of a row, padded; kLatent: the value is the
+// key row's front.  T: the inputs' type; kF8: the cache holds e4m3.
+template <int T, bool kF8, int KD, int VD, bool kLatent>
+__global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decode_kernel(Args a, Plan plan) {
+  typedef typename Elem<T>::vec8 vec8;
+  constexpr int NCK = KD / 8, NCV = VD / 8;                      // 16-byte chunks of a row in LDS
+  constexpr int LK = kTile * NCK / 64, LV = kLatent ? 0 : kTile * NCV / 64;   // loads of a lane for a tile
+  constexpr int kKeyBytes = kTile * KD * 2, kTileBytes = kKeyBytes + (kLatent ? 0 : kTile * VD * 2);
+  constexpr int kPad = VD + 4;                                   // floats of a row in the final exchange
+  constexpr int kWaveBytes = ((kTileBytes > kRows * kPad * 4 ? kTileBytes : kRows * kPad * 4) + 1023) / 1024 * 1024;
+  __shared__ __attribute__((aligned(16))) char s_tile[kWaves * kWaveBytes];
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = lane & 15, quad = lane >> 4;
+  const int32_t groups = (a.group + kRows - 1) / kRows;
+  const int32_t sub = blockIdx.x % (a.kv_heads * groups), item = blockIdx.x / (a.kv_heads * groups);
+  const int32_t kv_head = sub % a.kv_heads, first_row = sub / a.kv_heads * kRows;
+  Item it = {item, 0, 1, 0};
+  if (plan.chunks > 0) {
+    if (!find_item(a, plan, item, &it)) return;
+    if (sub == 0 && it.chunk == 0 && threadIdx.x == 0) plan.cut[it.request] = make_int2(it.of, it.slot);
+  }
+  const int32_t pos = clamped_len(a, it.request) - 1;
+  const Span span = key_span(a, pos, pos);
+  int32_t begin = 0, end = span.count;
+  if (it.of > 1) {
+    const int32_t size = ((span.count + it.of - 1) / it.of + kTile - 1) / kTile * kTile;
+    begin = it.chunk * size < span.count ? it.chunk * size : span.count;
+    end = begin + size < span.count ? begin + size : span.count;
+  }
+
+  // the query rows: lane (row, quad) holds elements quad * 8 .. + 7 of every 32
+  vec8 q[KD / 32];
+  {
+    const int32_t h = first_row + row;
+    const char* at = static_cast<const char*>(a.q) +
+                     ((int64_t)it.request * a.q_stride + (int64_t)(kv_head * a.group + h) * a.head_dim) * 2;
+#pragma unroll
+    for (int s = 0; s < KD / 32; ++s) {
+      const int d = s * 32 + quad * 8;
+      union {
+        uint4v w;
+        vec8 v;
+      } u;
+      u.w = uint4v{0, 0, 0, 0};
+      if (h < a.group && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(at + 2 * d);
+      q[s] = u.v;
+    }
+  }
+
+  const int32_t* table = a.tables + (int64_t)it.request * a.bt_stride;
+  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
+  char* tile = s_tile + wave * kWaveBytes;
+  const int32_t key_chunks = a.head_dim / 8;                     // of 8 elements
+  const int32_t value_chunks = kLatent ? 0 : a.value_dim / 8;
+  constexpr int kChunkBytes = kF8 ? 8 : 16;
+  typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
+
+  if (key_chunks < NCK) {                                        // padding stays zero: loads leave it alone
+#pragma unroll
+    for (int i = 0; i < kWaveBytes / 1024; ++i)
+      *reinterpret_cast<uint4v*>(tile + (i * 64 + lane) * 16) = uint4v{0, 0, 0, 0};
+  }
+
+  float4v acc[VD / 16];
+#pragma unroll
+  for (int t = 0; t < VD / 16; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  // offset of key (tile i's first + lane % 32), -1 where there is none
+  auto locate = [&](int32_t first) -> int64_t {
+    const int32_t v = first + (lane & 31);
+    return v < end ? row_offset(a, table, key_position(span, v)) : -1;
+  };
+  Raw rk[LK], rv[LV > 0 ? LV : 1];
+  auto fetch = [&](int64_t off) {
+    const uint32_t safe_lo = off < 0 ? 0u : (uint32_t)off, safe_hi = off < 0 ? 0u : (uint32_t)(off >> 32);
+#pragma unroll
+    for (int i = 0; i < LK; ++i) {
+      const int place = i * 64 + lane, r = place / NCK, c = (place - r * NCK) ^ swizzle<NCK>(r);
+      const char* from = cache + ((int64_t)((uint64_t)(uint32_t)__shfl((int)safe_hi, r, 64) << 32 | (uint32_t)__shfl((int)safe_lo, r, 64)));
+      if (c < key_chunks) rk[i] = *reinterpret_cast<const Raw*>(from + c * kChunkBytes);
+    }
+#pragma unroll
+    for (int i = 0; i < LV; ++i) {
+      const int place = i * 64 + lane, r = place / NCV, c = (place - r * NCV) ^ swizzle<NCV>(r);
+      const char* from = cache + a.value_bytes + ((int64_t)((uint64_t)(uint32_t)__shfl((int)safe_hi, r, 64) << 32 | (uint32_t)__shfl((int)safe_lo, r, 64)));
+      if (c < value_chunks) rv[i] = *reinterpret_cast<const Raw*>(from + c * kChunkBytes);
+    }
+  };
+  // registers to LDS; rows without a key as zeros, whatever their place holds
+  auto put = [&](uint32_t there) {
+#pragma unroll
+    for (int i = 0; i < LK; ++i) {
+      const int place = i * 64 + lane, r = place / NCK, c = (place - r * NCK) ^ swizzle<NCK>(r);
+      uint4v w;
+      if constexpr (kF8) w = widen<T>(rk[i]);
+      else w = rk[i];
+      if (!(there >> r & 1)) w = uint4v{0, 0, 0, 0};
+      if (c < key_chunks) *reinterpret_cast<uint4v*>(tile + place * 16) = w;
+    }
+#pragma unroll
+    for (int i = 0; i < LV; ++i) {
+      const int place = i * 64 + lane, r = place / NCV, c = (place - r * NCV) ^ swizzle<NCV>(r);
+      uint4v w;
+      if constexpr (kF8) w = widen<T>(rv[i]);
+      else w = rv[i];
+      if (!(there >> r & 1)) w = uint4v{0, 0, 0, 0};
+      if (c < value_chunks) *reinterpret_cast<uint4v*>(tile + kKeyBytes + place * 16) = w;
+    }
+  };
+
+  int32_t first = begin + wave * kTile;
+  if (first < end) {
+    int64_t off = locate(first);
+    fetch(off);
+    int64_t off_next = locate(first + kStep);
+    for (; first < end; first += kStep) {
+      const uint32_t there = (uint32_t)__ballot(off >= 0);       // bit k: key k of the tile is one
+      put(there);
+      wave_fence();
+      off = off_next;
+      if (first + kStep < end) {
+        fetch(off);
+        off_next = locate(first + 2 * kStep);
+      }
+      // scores of 2 x 16 keys: lane (row, quad) gets keys 4 quad .. + 3 of each half
+      float4v x[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        x[b] = float4v{0.f, 0.f, 0.f, 0.f};
+        const int r = b * 16 + row;
+#pragma unroll
+        for (int s = 0; s < KD / 32; ++s) {
+          const vec8 k = *reinterpret_cast<const vec8*>(tile + (r * NCK + ((s * 4 + quad) ^ swizzle<NCK>(r))) * 16);
+          x[b] = Elem<T>::mfma16(k, q[s], x[b]);
+        }
+      }
+      if (there != 0xffffffffu) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(there >> (b * 16 + quad * 4 + i) & 1)) x[b][i] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                        fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+      top = max_quarters(top) * a.scale;
+      if (__any(top > m)) {                                      // some row's maximum rises
+        const float up = fmaxf(m, top), fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
+        m = up;
+        l *= fall;
+#pragma unroll
+        for (int t = 0; t < VD / 16; ++t) acc[t] *= fall;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      vec8 p;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], a.scale, -base));
+          l += w;
+          p[b * 4 + i] = (typename Elem<T>::type)w;              // in [0, 1]: rounded for the matrix units, its sum is not
+        }
+      // values by columns: lane (d, quad) takes keys 4 quad .. + 3 of each half, as the weights lie
+      const char* values = tile + (kLatent ? 0 : kKeyBytes);
+#pragma unroll
+      for (int t = 0; t < VD / 16; ++t) {
+        union {
+          uint2v h[2];
+          vec8 v;
+        } u;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int r = b * 16 + quad * 4 + (row >> 2), c = t * 2 + (row >> 1 & 1);
+          constexpr int NC = kLatent ? NCK : NCV;
+          u.h[b] = read_transposed(values + (r * NC + (c ^ swizzle<NC>(r))) * 16 + (row & 1) * 8);
+        }
+        acc[t] = Elem<T>::mfma16(u.v, p, acc[t]);
+      }
+      wave_fence();
+    }
+  }
+
+  // the four waves' parts join in LDS
+  l = sum_quarters(l);
+  wave_fence();
+  float* mine = reinterpret_cast<float*>(tile);
+#pragma unroll
+  for (int t = 0; t < VD / 16; ++t) *reinterpret_cast<float4v*>(mine + row * kPad + t * 16 + quad * 4) = acc[t];
+  if (quad == 0) {
+    s_m[wave][row] = m;
+    s_l[wave][row] = l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kRows * (VD / 4); i += kThreads) {
+    const int r = i / (VD / 4), d = (i - r * (VD / 4)) * 4;
+    if (first_row + r >= a.group || d >= a.value_dim) continue;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    float4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][r] - base);
+      if (s_m[w][r] == -INFINITY) continue;                      // no key, or none that counts
+      sum += f * s_l[w][r];
+      o += *reinterpret_cast<const float4v*>(s_tile + w * kWaveBytes + (r * kPad + d) * 4) * f;
+    }
+    const int32_t head = kv_head * a.group + first_row + r;
+    if (it.of > 1) {
+      const int64_t at = ((int64_t)(it.slot + it.chunk) * a.kv_heads + kv_head) * a.group + first_row + r;
+      float* out = plan.part + at * a.value_dim + d;
+      for (int e = 0; e < 4; ++e)
+        if (d + e < a.value_dim) out[e] = o[e];
+      if (d == 0) plan.part_ml[at] = float2v{top, sum};
+    } else {
+      const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
+      typename Elem<T>::type* out =
+          static_cast<typename Elem<T>::type*>(a.out) + (int64_t)it.request * a.out_stride + (int64_t)head * a.value_dim + d;
+      for (int e = 0; e < 4; ++e)
+        if (d + e < a.value_dim) out[e] = (typename Elem<T>::type)(sum == 0.f ? 0.f : o[e] * inv);
+      if (a.lse && d == 0)
+        a.lse[(int64_t)it.request * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+}
+
+// Requests of several chunks: one workgroup per (request, query head).
+template <int T>
+__global__ __launch_bounds__(64) void kv_attention_join_kernel(Args a, Plan plan) {
+  const int32_t r = blockIdx.x / a.num_heads, head = blockIdx.x - r * a.num_heads;
+  const int2 cut = plan.cut[r];
+  if (cut.x <= 1) return;
+  const int64_t step = (int64_t)a.kv_heads * a.group;
+  const int64_t at = (int64_t)cut.y * step + head;
+  float top = -INFINITY;
+  for (int32_t k = threadIdx.x; k < cut.x; k += 64) top = fmaxf(top, plan.part_ml[at + k * step][0]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  const float base = top == -INFINITY ? 0.f : top;
+  for (int32_t d = threadIdx.x; d < a.value_dim; d += 64) {
+    float o = 0.f, sum = 0.f;
+    for (int32_t k = 0; k < cut.x; ++k) {
+      const float2v ml = plan.part_ml[at + k * step];
+      if (ml[0] == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+      sum += f * ml[1];
+      o += f * plan.part[(at + k * step) * a.value_dim + d];
+    }
+    const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
+    static_cast<typename Elem<T>::type*>(a.out)[(int64_t)r * a.out_stride + (int64_t)head * a.value_dim + d] =
+        (typename Elem<T>::type)(sum == 0.f ? 0.f : o * inv);
+    if (a.lse && d == 0)
+      a.lse[(int64_t)r * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+constexpr int kBusy = 1024;              // workgroups that the chunks are cut for
+
+int32_t units(const Args& a) { return a.kv_heads * ((a.group + kRows - 1) / kRows); }
+
+int32_t wanted_chunks(const Args& a) {
+  const int64_t seen = (int64_t)a.bt_stride * a.page_size;
+  const int64_t most = a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
+  if (most <= 2 * kStep) return 0;
+  const int32_t c = (kBusy + units(a) - 1) / units(a);
+  return c;
+}
+
+int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
+
+template <int T, bool kF8>
+void launch(const Args& a, const Plan& p, hipStream_t stream) {
+  const int64_t items = p.chunks > 0 ? (int64_t)p.chunks + a.num_reqs : a.num_reqs;
+  const dim3 grid((unsigned)(items * units(a))), block(kThreads);
+  const bool latent = a.value_bytes == 0;
+#define TOPKV_DECODE(KD, VD, LATENT) \
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_decode_kernel<T, kF8, KD, VD, LATENT>), grid, block, 0, stream, a, p)
+  if (latent) {
+    if (a.head_dim <= 128) TOPKV_DECODE(128, 128, true);
+    else TOPKV_DECODE(576, 512, true);
+  } else {
+    if (a.head_dim <= 64) TOPKV_DECODE(64, 64, false);
+    else if (a.head_dim <= 128) TOPKV_DECODE(128, 128, false);
+    else TOPKV_DECODE(256, 256, false);
+  }
+#undef TOPKV_DECODE
+  if (p.chunks > 0)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)(a.num_reqs * a.num_heads)), dim3(64), 0,
+                       stream, a, p);
+}
+
+}  // namespace
+
+bool decode_takes(const Args& a) {
+  const int64_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
+  const bool latent = a.value_bytes == 0;
+  if (a.head_dim % 8 != 0 || (latent ? a.head_dim > 576 || a.value_dim > 512 : a.head_dim > 256)) return false;
+  if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
+  const int64_t items = (int64_t)kBusy + a.num_reqs;
+  return items * units(a) <= INT32_MAX;
+}
+
+int64_t decode_workspace(const Args& a) {
+  const int32_t chunks = wanted_chunks(a);
+  if (chunks == 0) return 0;
+  const int64_t rows = 2 * (int64_t)chunks * a.kv_heads * a.group;
+  return up16(rows * a.value_dim * 4) + up16(rows * 8) + up16((int64_t)a.num_reqs * 8);
+}
+
+topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream) {
+  Plan p = {};
+  p.chunks = wanted_chunks(a);
+  if (p.chunks > 0) {
+    p.slots = 2 * p.chunks;
+    const int64_t rows = (int64_t)p.slots * a.kv_heads * a.group;
+    char* at = static_cast<char*>(workspace);
+    p.part = reinterpret_cast<float*>(at);
+    at += up16(rows * a.value_dim * 4);
+    p.part_ml = reinterpret_cast<float2v*>(at);
+    at += up16(rows * 8);
+    p.cut = reinterpret_cast<int2*>(at);
+  }
+  if (a.kv_dtype == TOPKV_FP8_E4M3) {
+    if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, p, stream);
+    else launch<TOPKV_FP16, true>(a, p, stream);
+  } else if (a.dtype == TOPKV_BF16) {
+    launch<TOPKV_BF16, false>(a, p, stream);
+  } else {
+    launch<TOPKV_FP16, false>(a, p, stream);
+  }
+  return hipGetLastError() == hipSuccess ? TOPKV_OK : TOPKV_ERR_LAUNCH;
+}
+
+}  // namespace topkv_attend

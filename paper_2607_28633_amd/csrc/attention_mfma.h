@@ -1,0 +1,118 @@
+// attention_mfma.h - types, matrix instructions and cross-lane steps of the
+// matrix-unit attention kernels.
+//
+// Both kernels compute the transposed products: scores^T = K Q^T and
+// out^T += V^T P^T, so that a query row is a column of every accumulator and
+// its maximum, sum and scale live in the lanes that hold the column.  The
+// scores' accumulator layout (4 consecutive keys per lane) is also a valid
+// layout of the second product's operand once both sides number the keys the
+// same way, so the weights never leave their registers.
+#ifndef TOPKV_ATTENTION_MFMA_H_
+#define TOPKV_ATTENTION_MFMA_H_
+
+#include "attention.h"
+
+namespace topkv_attend {
+
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef unsigned int uint2v __attribute__((ext_vector_type(2)));
+typedef unsigned int uint4v __attribute__((ext_vector_type(4)));
+
+template <int T> struct Elem;
+template <> struct Elem<TOPKV_BF16> {
+  typedef __bf16 type;
+  typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ float4v mfma16(vec8 a, vec8 b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float16v mfma32(vec8 a, vec8 b, float16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  // two e4m3 values (exact in either 16-bit type)
+  template <bool kHigh> static __device__ __forceinline__ vec2 from_fp8(uint32_t w) {
+    return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHigh);
+  }
+};
+template <> struct Elem<TOPKV_FP16> {
+  typedef _Float16 type;
+  typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ float4v mfma16(vec8 a, vec8 b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float16v mfma32(vec8 a, vec8 b, float16v c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+  template <bool kHigh> static __device__ __forceinline__ vec2 from_fp8(uint32_t w) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHigh);
+  }
+};
+
+// Eight e4m3 values as eight of T.
+template <int T>
+__device__ __forceinline__ uint4v widen(uint2v w) {
+  union {
+    typename Elem<T>::vec2 h[4];
+    uint4v v;
+  } u;
+  u.h[0] = Elem<T>::template from_fp8<false>(w[0]);
+  u.h[1] = Elem<T>::template from_fp8<true>(w[0]);
+  u.h[2] = Elem<T>::template from_fp8<false>(w[1]);
+  u.h[3] = Elem<T>::template from_fp8<true>(w[1]);
+  return u.v;
+}
+
+// Rows of NC 16-byte chunks in LDS: chunk c of row r is stored at place
+// c ^ swizzle(r).  Both reads, 16 rows of one chunk and 4 rows of 4 chunks,
+// then spread over all 64 banks (16 chunks): rows r, r + 1, .. start 16
+// chunks apart (NC % 16 == 0) or 8 chunks apart (NC % 16 == 8).
+template <int NC>
+__device__ __forceinline__ int swizzle(int r) {
+  static_assert(NC % 8 == 0, "a row is whole groups of 8 chunks");
+  if constexpr (NC % 16 == 0) return (r & 3) << 2 | (r >> 2 & 3);
+  else return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+}
+
+// Four rows of 16 16-bit values, 4 of them given by each of 16 lanes (row
+// lane / 4), returned by columns: lane i has column i.
+__device__ __forceinline__ uint2v read_transposed(const char* lds) {
+  typedef short4v __attribute__((address_space(3))) * P;
+  union {
+    short4v s;
+    uint2v v;
+  } u;
+  u.s = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds));
+  return u.v;
+}
+
+// Maximum and sum over the lanes that differ in bit 5, and in bits 4 and 5.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// The order of this wave's LDS accesses, for the compiler (the hardware keeps it).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+}  // namespace topkv_attend
+
+#endif  // TOPKV_ATTENTION_MFMA_H_
