@@ -673,8 +673,8 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
  * units, others on a slower general kernel.  Errors: TOPKV_ERR_INVALID_ARG for bad
  * descriptors, options, null pointers or a short or misaligned workspace,
  * TOPKV_ERR_UNSUPPORTED for head_dim above 1024, more than
- * TOPKV_MAX_BATCH_REQS requests, bt_stride * page_size of 2^30 or more or
- * 2^31 (token, head) rows, TOPKV_ERR_LAUNCH.  Does not synchronise and can be
+ * TOPKV_MAX_BATCH_REQS requests, bt_stride * page_size of 2^30 or more,
+ * num_reqs * bt_stride * page_size of 2^31 or more or 2^31 (token, head) rows, TOPKV_ERR_LAUNCH.  Does not synchronise and can be
  * captured into a graph. */
 topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_attention_t* attn,
                                       int32_t num_reqs, const int32_t* seq_lens, const void* q, void* out,

@@ -25,6 +25,7 @@ struct Args {
   int64_t value_bytes;        // from a key row to its value row
   int64_t q_stride, out_stride;
   int32_t page_size, bt_stride, num_reqs, total_q;
+  uint32_t page_mul, page_shift;   // position / page_size = position * page_mul >> page_shift, positions below 2^30
   int32_t num_heads, kv_heads, group;
   int32_t head_dim, value_dim;
   int32_t window, sinks;
@@ -68,10 +69,16 @@ __device__ __forceinline__ bool sees(const Args& a, int32_t pos, int32_t j) {
   return j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
 }
 
+// j / page_size: with l = ceil(log2(page_size)) the multiplier ceil(2^(30 + l) / page_size) is at most 2^30 / page_size
+// too large in 2^(30 + l), which no j below 2^30 can feel.
+__device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t j) {
+  return (uint32_t)((uint64_t)j * a.page_mul >> a.page_shift);
+}
+
 // Byte offset of position j's row from a.cache, or -1 when its page lies
 // outside the pool.
 __device__ __forceinline__ int64_t row_offset(const Args& a, const int32_t* __restrict__ table, int32_t j) {
-  const uint32_t page = (uint32_t)j / (uint32_t)a.page_size;
+  const uint32_t page = page_of(a, (uint32_t)j);
   const int32_t e = table[page];
   if (e < 0 || e >= a.num_pages) return -1;
   return (int64_t)e * a.page_bytes + (int64_t)((uint32_t)j - page * (uint32_t)a.page_size) * a.slot_bytes;

@@ -157,7 +157,7 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
     return TOPKV_ERR_INVALID_ARG;
   if (num_reqs < 0 || total_q < 0) return TOPKV_ERR_INVALID_ARG;
   if (p.head_dim > 1024 || num_reqs > TOPKV_MAX_BATCH_REQS || (int64_t)v->bt_stride * p.page_size >= (1 << 30) ||
-      (int64_t)total_q * t->num_heads > INT32_MAX)
+      (int64_t)num_reqs * v->bt_stride * p.page_size > INT32_MAX || (int64_t)total_q * t->num_heads > INT32_MAX)
     return TOPKV_ERR_UNSUPPORTED;
   const int64_t elem = p.elem_bytes, plane = (int64_t)p.page_size * p.num_heads * p.head_dim * elem;
   const bool head_major = v->layout == TOPKV_LAYOUT_POOL_HEAD_MAJOR;
@@ -170,6 +170,10 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
   a->tables = v->block_tables;
   a->num_pages = p.num_pages;
   a->page_size = p.page_size;
+  int log2 = 0;
+  while ((int64_t)1 << log2 < p.page_size) ++log2;
+  a->page_shift = 30 + log2;
+  a->page_mul = (uint32_t)((((uint64_t)1 << a->page_shift) + p.page_size - 1) / p.page_size);
   a->bt_stride = v->bt_stride;
   a->num_reqs = num_reqs;
   a->total_q = total_q;

@@ -8,10 +8,12 @@
 // The four waves of a workgroup take tiles in turn and join at the end.
 //
 // Few requests would leave most of the GPU idle, uneven ones would wait for
-// the longest: the visible tokens of the whole batch are cut into chunks of
-// one size, as many as keep the GPU busy, and requests of several chunks are
-// joined by a second kernel from partial results in 32 bits.  The cut follows
-// the lengths on the device, not the width of the tables.
+// the longest: the tiles of the whole batch, request after request, are cut
+// into shares of one size, one for each workgroup that fits the GPU at once.
+// A share may hold the end of one request, some whole ones and the start of
+// another; requests cut into pieces are joined by a second kernel from partial
+// results in 32 bits.  The cut follows the lengths on the device, not the
+// width of the tables.
 #include "attention_internal.h"
 #include "attention_mfma.h"
 
@@ -25,81 +27,78 @@ constexpr int kTile = 32;                // keys of one wave's tile
 constexpr int kRows = 16;                // query rows of a workgroup
 constexpr int kStep = kTile * kWaves;    // keys of the workgroup's tiles
 
+constexpr int kLeast = 8;                // tiles of a share, at least: smaller pieces cost more to join than they save
+constexpr int kSingle = 512;             // longest visible length that is never cut (one launch, no join)
+
+// Shares, by the key width: as many workgroups as 256 CUs hold at once by their LDS (64 KiB at 128 elements, 128 KiB
+// at 256).  131072 tokens, 8 heads of 128: 512 shares 108 us, 768 114, 1024 113, 2048 121; heads of 64, of which four
+// workgroups fit a CU, 512 118 us, 768 123, 1024 131.
+constexpr int resident(int KD) { return KD <= 128 ? 512 : 256; }
+
 struct Plan {
-  int32_t chunks;      // wanted over all requests; 0: one per request, whatever its length
-  int32_t slots;       // partial results that fit (requests of one chunk need none)
-  float* part;         // [slot][kv head][row of the group][value_dim]
-  float2v* part_ml;    // [slot][kv head][row of the group]: maximum and sum
-  int2* cut;           // [request]: chunks, first slot
+  int32_t shares;      // wanted; 0: one per request, whatever its length
+  float* part;         // [2 * share + 1 for a request's first piece][kv head][row of the group][value_dim]
+  float2v* part_ml;    // the same without value_dim: maximum and sum
+  int2* cut;           // [request]: pieces, share of the first
 };
 
-struct Item {
-  int32_t request, chunk, of, slot;      // slot: of the request's first chunk
+struct Share {
+  int32_t request;     // of the first tile; -1: the share is empty
+  int32_t base;        // number of that request's first tile
+  int32_t size;        // tiles of a share
+  int32_t total;       // tiles of the batch
 };
 
-__device__ __forceinline__ int32_t decode_count(const Args& a, int32_t r) {
-  const int32_t p = clamped_len(a, r) - 1;
-  return key_span(a, p, p).count;
+// Every request has at least one tile, so that those of no tokens are written too.
+__device__ __forceinline__ int32_t tiles_of(const Args& a, int32_t r) {
+  const int32_t p = clamped_len(a, r) - 1, n = key_span(a, p, p).count;
+  return n < 1 ? 1 : (n + kTile - 1) / kTile;
 }
 
-// Which request and chunk item number `item` is; false past the last.
-__device__ bool find_item(const Args& a, const Plan& p, int32_t item, Item* got) {
-  __shared__ int64_t s_total[kWaves];
-  __shared__ int32_t s_items[kWaves], s_slots[kWaves];
-  __shared__ Item s_got;
+__device__ Share find_share(const Args& a, int32_t shares, int32_t share) {
+  __shared__ int32_t s_sum[kWaves];
+  __shared__ Share s_got;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t per = (a.num_reqs + kThreads - 1) / kThreads;
   const int32_t lo = threadIdx.x * per, hi = lo + per < a.num_reqs ? lo + per : a.num_reqs;
-  int64_t total = 0;
-  for (int32_t r = lo; r < hi; ++r) total += decode_count(a, r);
-#pragma unroll
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d, 64);
-  if (lane == 0) s_total[wave] = total;
-  if (threadIdx.x == 0) s_got.request = -1;
-  __syncthreads();
-  total = 0;
-  for (int i = 0; i < kWaves; ++i) total += s_total[i];
-  int64_t size = (total + p.chunks - 1) / p.chunks;
-  size = size < 2 * kStep ? 2 * kStep : (size + kStep - 1) / kStep * kStep;
-  int32_t items = 0, slots = 0;
-  for (int32_t r = lo; r < hi; ++r) {
-    const int32_t n = (int32_t)((decode_count(a, r) + size - 1) / size), c = n < 1 ? 1 : n;
-    items += c;
-    slots += c > 1 ? c : 0;
-  }
-  int32_t items_inc = items, slots_inc = slots;
+  int32_t mine = 0;
+  for (int32_t r = lo; r < hi; ++r) mine += tiles_of(a, r);
+  int32_t inc = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int32_t x = __shfl_up(items_inc, d, 64), y = __shfl_up(slots_inc, d, 64);
-    if (lane >= d) items_inc += x, slots_inc += y;
+    const int32_t x = __shfl_up(inc, d, 64);
+    if (lane >= d) inc += x;
   }
-  if (lane == 63) s_items[wave] = items_inc, s_slots[wave] = slots_inc;
+  if (lane == 63) s_sum[wave] = inc;
+  if (threadIdx.x == 0) s_got.request = -1;
   __syncthreads();
-  int32_t at = items_inc - items, slot = slots_inc - slots;
-  for (int i = 0; i < wave; ++i) at += s_items[i], slot += s_slots[i];
-  if (item >= at && item < at + items) {
-    for (int32_t r = lo; r < hi; ++r) {
-      const int32_t n = (int32_t)((decode_count(a, r) + size - 1) / size), c = n < 1 ? 1 : n;
-      if (item < at + c) {
-        s_got.request = r;
-        s_got.chunk = item - at;
-        s_got.of = c;
-        s_got.slot = slot;
-        break;
-      }
-      at += c;
-      slot += c > 1 ? c : 0;
-    }
+  int32_t base = inc - mine, total = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) base += s_sum[i];
+    total += s_sum[i];
+  }
+  int32_t size = (total + shares - 1) / shares;
+  size = size < kLeast ? kLeast : size;
+  const int32_t first = share * size;
+  if (first >= base && first < base + mine) {
+    int32_t r = lo;
+    for (int32_t n = tiles_of(a, r); first >= base + n; n = tiles_of(a, ++r)) base += n;
+    s_got.request = r;
+    s_got.base = base;
   }
   __syncthreads();
-  *got = s_got;
-  return got->request >= 0;
+  Share got = s_got;
+  got.size = size;
+  got.total = total;
+  return got;
 }
 
 // KD, VD: key and value elements of a row, padded; kLatent: the value is the
 // key row's front.  T: the inputs' type; kF8: the cache holds e4m3.
-template <int T, bool kF8, int KD, int VD, bool kLatent>
-__global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decode_kernel(Args a, Plan plan) {
+// kCut: the batch is cut into shares; otherwise a workgroup takes one request.
+template <int T, bool kF8, int KD, int VD, bool kLatent, bool kCut>
+__global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_decode_kernel(Args a, Plan plan) {
   typedef typename Elem<T>::vec8 vec8;
   constexpr int NCK = KD / 8, NCV = VD / 8;                      // 16-byte chunks of a row in LDS
   constexpr int LK = kTile * NCK / 64, LV = kLatent ? 0 : kTile * NCV / 64;   // loads of a lane for a tile
@@ -112,20 +111,47 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane & 15, quad = lane >> 4;
   const int32_t groups = (a.group + kRows - 1) / kRows;
-  const int32_t sub = blockIdx.x % (a.kv_heads * groups), item = blockIdx.x / (a.kv_heads * groups);
+  // Eight items side by side over the eight XCDs, an item's KV heads one after the other on one XCD: with the
+  // heads side by side each XCD would read a narrow column of the cache through a few channels of its L2.
+  const int32_t units = a.kv_heads * groups, eight = blockIdx.x / (8 * units), within = blockIdx.x - eight * 8 * units;
+  const int32_t share = eight * 8 + (within & 7), sub = within >> 3;
   const int32_t kv_head = sub % a.kv_heads, first_row = sub / a.kv_heads * kRows;
-  Item it = {item, 0, 1, 0};
-  if (plan.chunks > 0) {
-    if (!find_item(a, plan, item, &it)) return;
-    if (sub == 0 && it.chunk == 0 && threadIdx.x == 0) plan.cut[it.request] = make_int2(it.of, it.slot);
+  char* tile = s_tile + wave * kWaveBytes;
+  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
+  const int32_t key_chunks = a.head_dim / 8;                     // of 8 elements
+  const int32_t value_chunks = kLatent ? 0 : a.value_dim / 8;
+  constexpr int kChunkBytes = kF8 ? 8 : 16;
+  typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
+
+  Share sh = {share, 0, 0, 0};
+  int32_t tile_at = 0, tile_end = 1;                             // tiles of the batch; uncut: the request as one
+  if constexpr (kCut) {
+    sh = find_share(a, plan.shares, share);
+    if (sh.request < 0) return;
+    tile_at = share * sh.size;
+    tile_end = tile_at + sh.size < sh.total ? tile_at + sh.size : sh.total;
+  } else {
+    if (share >= a.num_reqs) return;
   }
-  const int32_t pos = clamped_len(a, it.request) - 1;
+
+  for (int32_t request = sh.request; tile_at < tile_end; ++request) {
+  const int32_t pos = clamped_len(a, request) - 1;
   const Span span = key_span(a, pos, pos);
   int32_t begin = 0, end = span.count;
-  if (it.of > 1) {
-    const int32_t size = ((span.count + it.of - 1) / it.of + kTile - 1) / kTile * kTile;
-    begin = it.chunk * size < span.count ? it.chunk * size : span.count;
-    end = begin + size < span.count ? begin + size : span.count;
+  bool whole = true, opens = false;
+  if constexpr (kCut) {
+    const int32_t tiles = span.count < 1 ? 1 : (span.count + kTile - 1) / kTile, from = tile_at - sh.base;
+    const int32_t to = tile_end - sh.base < tiles ? tile_end - sh.base : tiles;
+    opens = from == 0;
+    whole = opens && to == tiles;
+    begin = from * kTile;
+    end = to * kTile < span.count ? to * kTile : span.count;
+    if (opens && sub == 0 && threadIdx.x == 0)
+      plan.cut[request] = make_int2((sh.base + tiles - 1) / sh.size - share + 1, share);
+    tile_at = sh.base + to;
+    sh.base += tiles;
+  } else {
+    tile_at = tile_end;
   }
 
   // the query rows: lane (row, quad) holds elements quad * 8 .. + 7 of every 32
@@ -133,7 +159,7 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
   {
     const int32_t h = first_row + row;
     const char* at = static_cast<const char*>(a.q) +
-                     ((int64_t)it.request * a.q_stride + (int64_t)(kv_head * a.group + h) * a.head_dim) * 2;
+                     ((int64_t)request * a.q_stride + (int64_t)(kv_head * a.group + h) * a.head_dim) * 2;
 #pragma unroll
     for (int s = 0; s < KD / 32; ++s) {
       const int d = s * 32 + quad * 8;
@@ -147,14 +173,7 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
     }
   }
 
-  const int32_t* table = a.tables + (int64_t)it.request * a.bt_stride;
-  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
-  char* tile = s_tile + wave * kWaveBytes;
-  const int32_t key_chunks = a.head_dim / 8;                     // of 8 elements
-  const int32_t value_chunks = kLatent ? 0 : a.value_dim / 8;
-  constexpr int kChunkBytes = kF8 ? 8 : 16;
-  typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
-
+  const int32_t* table = a.tables + (int64_t)request * a.bt_stride;
   if (key_chunks < NCK) {                                        // padding stays zero: loads leave it alone
 #pragma unroll
     for (int i = 0; i < kWaveBytes / 1024; ++i)
@@ -166,10 +185,17 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
   for (int t = 0; t < VD / 16; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  // offset of key (tile i's first + lane % 32), -1 where there is none
-  auto locate = [&](int32_t first) -> int64_t {
+  // The table entry of key (tile i's first + lane % 32) is asked for two tiles ahead and before the rows of the
+  // next tile, so that its wait, a tile later, waits for nothing younger.
+  auto ask = [&](int32_t first) -> int32_t {
     const int32_t v = first + (lane & 31);
-    return v < end ? row_offset(a, table, key_position(span, v)) : -1;
+    return v < end ? table[page_of(a, (uint32_t)key_position(span, v))] : -1;
+  };
+  auto locate = [&](int32_t first, int32_t entry) -> int64_t {
+    const int32_t v = first + (lane & 31);
+    if (v >= end || entry < 0 || entry >= a.num_pages) return -1;
+    const uint32_t j = (uint32_t)key_position(span, v);
+    return (int64_t)entry * a.page_bytes + (int64_t)(j - page_of(a, j) * (uint32_t)a.page_size) * a.slot_bytes;
   };
   Raw rk[LK], rv[LV > 0 ? LV : 1];
   auto fetch = [&](int64_t off) {
@@ -211,17 +237,17 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
 
   int32_t first = begin + wave * kTile;
   if (first < end) {
-    int64_t off = locate(first);
+    int64_t off = locate(first, ask(first));
+    int32_t entry = ask(first + kStep);
     fetch(off);
-    int64_t off_next = locate(first + kStep);
     for (; first < end; first += kStep) {
       const uint32_t there = (uint32_t)__ballot(off >= 0);       // bit k: key k of the tile is one
       put(there);
       wave_fence();
-      off = off_next;
+      off = locate(first + kStep, entry);
       if (first + kStep < end) {
+        entry = ask(first + 2 * kStep);
         fetch(off);
-        off_next = locate(first + 2 * kStep);
       }
       // scores of 2 x 16 keys: lane (row, quad) gets keys 4 quad .. + 3 of each half
       float4v x[2];
@@ -310,75 +336,104 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_decod
       o += *reinterpret_cast<const float4v*>(s_tile + w * kWaveBytes + (r * kPad + d) * 4) * f;
     }
     const int32_t head = kv_head * a.group + first_row + r;
-    if (it.of > 1) {
-      const int64_t at = ((int64_t)(it.slot + it.chunk) * a.kv_heads + kv_head) * a.group + first_row + r;
-      float* out = plan.part + at * a.value_dim + d;
+    if (!whole) {
+      const int64_t slot = ((2 * (int64_t)share + opens) * a.kv_heads + kv_head) * a.group + first_row + r;
+      float* out = plan.part + slot * a.value_dim + d;
       for (int e = 0; e < 4; ++e)
         if (d + e < a.value_dim) out[e] = o[e];
-      if (d == 0) plan.part_ml[at] = float2v{top, sum};
+      if (d == 0) plan.part_ml[slot] = float2v{top, sum};
     } else {
       const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
       typename Elem<T>::type* out =
-          static_cast<typename Elem<T>::type*>(a.out) + (int64_t)it.request * a.out_stride + (int64_t)head * a.value_dim + d;
+          static_cast<typename Elem<T>::type*>(a.out) + (int64_t)request * a.out_stride + (int64_t)head * a.value_dim + d;
       for (int e = 0; e < 4; ++e)
         if (d + e < a.value_dim) out[e] = (typename Elem<T>::type)(sum == 0.f ? 0.f : o[e] * inv);
       if (a.lse && d == 0)
-        a.lse[(int64_t)it.request * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        a.lse[(int64_t)request * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
+  }
+  __syncthreads();                                               // the tiles' place is free again
   }
 }
 
-// Requests of several chunks: one workgroup per (request, query head).
+// Requests in pieces: one workgroup per (request, query head, 64 elements).
+// The pieces' weights first, then their sum with the pieces over the waves and
+// the elements over the lanes, so that no load waits for another.
+constexpr int kJoinWaves = 8;
+
 template <int T>
-__global__ __launch_bounds__(64) void kv_attention_join_kernel(Args a, Plan plan) {
+__global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Args a, Plan plan) {
+  __shared__ float s_weight[resident(128)], s_sum[kJoinWaves], s_part[kJoinWaves][64];
   const int32_t r = blockIdx.x / a.num_heads, head = blockIdx.x - r * a.num_heads;
   const int2 cut = plan.cut[r];
   if (cut.x <= 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t step = (int64_t)a.kv_heads * a.group;
-  const int64_t at = (int64_t)cut.y * step + head;
-  float top = -INFINITY;
-  for (int32_t k = threadIdx.x; k < cut.x; k += 64) top = fmaxf(top, plan.part_ml[at + k * step][0]);
+  const int64_t at = 2 * (int64_t)cut.y * step + head;            // piece k: slot 2 (first + k), the first one's next to it
+  const int32_t d = blockIdx.y * 64 + lane;
+  float top = -INFINITY;                                         // every wave over all chunks
+  for (int32_t k = lane; k < cut.x; k += 64) top = fmaxf(top, plan.part_ml[at + (k ? 2 * k : 1) * step][0]);
 #pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
   const float base = top == -INFINITY ? 0.f : top;
-  for (int32_t d = threadIdx.x; d < a.value_dim; d += 64) {
-    float o = 0.f, sum = 0.f;
-    for (int32_t k = 0; k < cut.x; ++k) {
-      const float2v ml = plan.part_ml[at + k * step];
-      if (ml[0] == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(ml[0] - base);
-      sum += f * ml[1];
-      o += f * plan.part[(at + k * step) * a.value_dim + d];
-    }
-    const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
-    static_cast<typename Elem<T>::type*>(a.out)[(int64_t)r * a.out_stride + (int64_t)head * a.value_dim + d] =
-        (typename Elem<T>::type)(sum == 0.f ? 0.f : o * inv);
-    if (a.lse && d == 0)
-      a.lse[(int64_t)r * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  float sum = 0.f;
+  for (int32_t k = threadIdx.x; k < cut.x; k += 64 * kJoinWaves) {
+    const float2v ml = plan.part_ml[at + (k ? 2 * k : 1) * step];
+    const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+    s_weight[k] = f;
+    sum += f * ml[1];
   }
+#pragma unroll
+  for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i, 64);
+  if (lane == 0) s_sum[wave] = sum;
+  __syncthreads();
+  float o = 0.f;
+  if (d < a.value_dim) {
+    const float* from = plan.part + at * a.value_dim + d;
+    const int64_t row = step * a.value_dim;
+#pragma unroll 8
+    for (int32_t k = wave; k < cut.x; k += kJoinWaves) o = fmaf(s_weight[k], from[(k ? 2 * k : 1) * row], o);
+  }
+  s_part[wave][lane] = o;
+  __syncthreads();
+  if (wave > 0) return;
+  sum = 0.f;
+  o = 0.f;
+  for (int w = 0; w < kJoinWaves; ++w) {
+    sum += s_sum[w];
+    o += s_part[w][lane];
+  }
+  if (d < a.value_dim)
+    static_cast<typename Elem<T>::type*>(a.out)[(int64_t)r * a.out_stride + (int64_t)head * a.value_dim + d] =
+        (typename Elem<T>::type)(sum == 0.f ? 0.f : o * (a.v_scale / sum));
+  if (a.lse && d == 0)
+    a.lse[(int64_t)r * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
-
-constexpr int kBusy = 1024;              // workgroups that the chunks are cut for
 
 int32_t units(const Args& a) { return a.kv_heads * ((a.group + kRows - 1) / kRows); }
 
-int32_t wanted_chunks(const Args& a) {
+int32_t wanted_shares(const Args& a) {
   const int64_t seen = (int64_t)a.bt_stride * a.page_size;
   const int64_t most = a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
-  if (most <= 2 * kStep) return 0;
-  const int32_t c = (kBusy + units(a) - 1) / units(a);
-  return c;
+  if (most <= kSingle) return 0;
+  const int32_t n = resident(a.head_dim) / units(a);
+  return n < 1 ? 1 : n;
 }
 
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 
 template <int T, bool kF8>
 void launch(const Args& a, const Plan& p, hipStream_t stream) {
-  const int64_t items = p.chunks > 0 ? (int64_t)p.chunks + a.num_reqs : a.num_reqs;
-  const dim3 grid((unsigned)(items * units(a))), block(kThreads);
+  const int64_t items = p.shares > 0 ? p.shares : a.num_reqs;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8 * units(a))), block(kThreads);
   const bool latent = a.value_bytes == 0;
-#define TOPKV_DECODE(KD, VD, LATENT) \
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_decode_kernel<T, kF8, KD, VD, LATENT>), grid, block, 0, stream, a, p)
+#define TOPKV_DECODE(KD, VD, LATENT)                                                                                         \
+  do {                                                                                                                       \
+    if (p.shares > 0)                                                                                                        \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_decode_kernel<T, kF8, KD, VD, LATENT, true>), grid, block, 0, stream, a, p);  \
+    else                                                                                                                     \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_decode_kernel<T, kF8, KD, VD, LATENT, false>), grid, block, 0, stream, a, p); \
+  } while (0)
   if (latent) {
     if (a.head_dim <= 128) TOPKV_DECODE(128, 128, true);
     else TOPKV_DECODE(576, 512, true);
@@ -388,9 +443,8 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
     else TOPKV_DECODE(256, 256, false);
   }
 #undef TOPKV_DECODE
-  if (p.chunks > 0)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)(a.num_reqs * a.num_heads)), dim3(64), 0,
-                       stream, a, p);
+  if (p.shares > 0)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)(a.num_reqs * a.num_heads), (unsigned)((a.value_dim + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, a, p);
 }
 
 }  // namespace
@@ -400,23 +454,22 @@ bool decode_takes(const Args& a) {
   const bool latent = a.value_bytes == 0;
   if (a.head_dim % 8 != 0 || (latent ? a.head_dim > 576 || a.value_dim > 512 : a.head_dim > 256)) return false;
   if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
-  const int64_t items = (int64_t)kBusy + a.num_reqs;
-  return items * units(a) <= INT32_MAX;
+  const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
+  return items * units(a) <= INT32_MAX && (int64_t)a.num_reqs * a.num_heads <= INT32_MAX;
 }
 
 int64_t decode_workspace(const Args& a) {
-  const int32_t chunks = wanted_chunks(a);
-  if (chunks == 0) return 0;
-  const int64_t rows = 2 * (int64_t)chunks * a.kv_heads * a.group;
+  const int32_t shares = wanted_shares(a);
+  if (shares == 0) return 0;
+  const int64_t rows = 2 * (int64_t)shares * a.kv_heads * a.group;
   return up16(rows * a.value_dim * 4) + up16(rows * 8) + up16((int64_t)a.num_reqs * 8);
 }
 
 topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream) {
   Plan p = {};
-  p.chunks = wanted_chunks(a);
-  if (p.chunks > 0) {
-    p.slots = 2 * p.chunks;
-    const int64_t rows = (int64_t)p.slots * a.kv_heads * a.group;
+  p.shares = wanted_shares(a);
+  if (p.shares > 0) {
+    const int64_t rows = 2 * (int64_t)p.shares * a.kv_heads * a.group;
     char* at = static_cast<char*>(workspace);
     p.part = reinterpret_cast<float*>(at);
     at += up16(rows * a.value_dim * 4);
