@@ -65,10 +65,6 @@ __device__ __forceinline__ Span key_span(const Args& a, int32_t first, int32_t l
 
 __device__ __forceinline__ int32_t key_position(const Span& s, int32_t i) { return i < s.head ? i : i - s.head + s.start; }
 
-__device__ __forceinline__ bool sees(const Args& a, int32_t pos, int32_t j) {
-  return j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
-}
-
 // j / page_size: with l = ceil(log2(page_size)) the multiplier ceil(2^(30 + l) / page_size) is at most 2^30 / page_size
 // too large in 2^(30 + l), which no j below 2^30 can feel.
 __device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t j) {
@@ -83,6 +79,25 @@ __device__ __forceinline__ int64_t row_offset(const Args& a, const int32_t* __re
   if (e < 0 || e >= a.num_pages) return -1;
   return (int64_t)e * a.page_bytes + (int64_t)((uint32_t)j - page * (uint32_t)a.page_size) * a.slot_bytes;
 }
+
+// One element of a row.
+template <int T> struct Load;
+template <> struct Load<TOPKV_BF16> {
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ float at(const char* p) {
+    return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+  }
+};
+template <> struct Load<TOPKV_FP16> {
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ float at(const char* p) { return (float)*reinterpret_cast<const _Float16*>(p); }
+};
+template <> struct Load<TOPKV_FP8_E4M3> {
+  static constexpr int kBytes = 1;
+  static __device__ __forceinline__ float at(const char* p) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)*reinterpret_cast<const uint8_t*>(p), 0);
+  }
+};
 
 }  // namespace topkv_attend
 

@@ -12,24 +12,6 @@ namespace topkv_attend {
 
 constexpr int kWaves = 4;
 
-template <int T> struct Load;
-template <> struct Load<TOPKV_BF16> {
-  static constexpr int kBytes = 2;
-  static __device__ __forceinline__ float at(const char* p) {
-    return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
-  }
-};
-template <> struct Load<TOPKV_FP16> {
-  static constexpr int kBytes = 2;
-  static __device__ __forceinline__ float at(const char* p) { return (float)*reinterpret_cast<const _Float16*>(p); }
-};
-template <> struct Load<TOPKV_FP8_E4M3> {
-  static constexpr int kBytes = 1;
-  static __device__ __forceinline__ float at(const char* p) {
-    return __builtin_amdgcn_cvt_f32_fp8((int)*reinterpret_cast<const uint8_t*>(p), 0);
-  }
-};
-
 template <int T>
 __device__ __forceinline__ void store(void* p, int64_t i, float v) {
   if constexpr (T == TOPKV_BF16) {
@@ -219,6 +201,7 @@ topkv_status_t attend(const topkv_view_t* cache, const topkv_attention_t* attn, 
   a.out = out;
   a.lse = lse;
   if (decode && decode_takes(a) && aligned(a)) return run_decode(a, workspace, stream);
+  if (!decode && prompt_takes(a) && aligned(a)) return run_prompt(a, stream);
   return run_general(a, stream);
 }
 

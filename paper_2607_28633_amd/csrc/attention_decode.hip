@@ -56,41 +56,21 @@ __device__ __forceinline__ int32_t tiles_of(const Args& a, int32_t r) {
 }
 
 __device__ Share find_share(const Args& a, int32_t shares, int32_t share) {
-  __shared__ int32_t s_sum[kWaves];
   __shared__ Share s_got;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t per = (a.num_reqs + kThreads - 1) / kThreads;
-  const int32_t lo = threadIdx.x * per, hi = lo + per < a.num_reqs ? lo + per : a.num_reqs;
-  int32_t mine = 0;
-  for (int32_t r = lo; r < hi; ++r) mine += tiles_of(a, r);
-  int32_t inc = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int32_t x = __shfl_up(inc, d, 64);
-    if (lane >= d) inc += x;
-  }
-  if (lane == 63) s_sum[wave] = inc;
   if (threadIdx.x == 0) s_got.request = -1;
-  __syncthreads();
-  int32_t base = inc - mine, total = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < wave) base += s_sum[i];
-    total += s_sum[i];
-  }
-  int32_t size = (total + shares - 1) / shares;
+  const auto tiles = [&](int32_t r) { return tiles_of(a, r); };
+  Scan n = scan_requests<kWaves>(a.num_reqs, tiles);
+  int32_t size = (n.total + shares - 1) / shares;
   size = size < kLeast ? kLeast : size;
   const int32_t first = share * size;
-  if (first >= base && first < base + mine) {
-    int32_t r = lo;
-    for (int32_t n = tiles_of(a, r); first >= base + n; n = tiles_of(a, ++r)) base += n;
-    s_got.request = r;
-    s_got.base = base;
+  if (first >= n.base && first < n.base + n.mine) {
+    s_got.request = n.find(first, tiles);
+    s_got.base = n.base;
   }
   __syncthreads();
   Share got = s_got;
   got.size = size;
-  got.total = total;
+  got.total = n.total;
   return got;
 }
 

@@ -107,10 +107,66 @@ __device__ __forceinline__ float sum_quarters(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// 16 bytes a lane from memory to LDS without registers in between: lane i's go
+// to lds + 16 i (lds the same in all lanes; lanes that are off write nothing).
+// The compiler does not see these loads: wait_loads() before their LDS is read.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // that m0 is a register of the target's own is why it is named
+__device__ __forceinline__ void load_to_lds(char* lds, const char* from) {
+  typedef char __attribute__((address_space(3))) * L;
+  const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(L)lds);
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // The order of this wave's LDS accesses, for the compiler (the hardware keeps it).
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+}
+
+// Running sums of a weight over the requests, each thread of the workgroup
+// with a run of neighbours; find() is for the thread whose run holds an item.
+struct Scan {
+  int32_t lo, hi;      // the thread's requests
+  int32_t base, mine;  // weight before them and of them
+  int32_t total;
+
+  // The request that item number `item` belongs to; base becomes its first item.
+  template <class F> __device__ int32_t find(int32_t item, F weight) {
+    int32_t r = lo;
+    for (int32_t w = weight(r); item >= base + w; w = weight(++r)) base += w;
+    return r;
+  }
+};
+
+template <int kWaves, class F>
+__device__ Scan scan_requests(int32_t num_reqs, F weight) {
+  __shared__ int32_t s_sum[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t per = (num_reqs + 64 * kWaves - 1) / (64 * kWaves);
+  Scan s;
+  s.lo = threadIdx.x * per;
+  s.hi = s.lo + per < num_reqs ? s.lo + per : num_reqs;
+  s.mine = 0;
+  for (int32_t r = s.lo; r < s.hi; ++r) s.mine += weight(r);
+  int32_t inc = s.mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int32_t x = __shfl_up(inc, d, 64);
+    if (lane >= d) inc += x;
+  }
+  if (lane == 63) s_sum[wave] = inc;
+  __syncthreads();
+  s.base = inc - s.mine;
+  s.total = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < wave) s.base += s_sum[i];
+    s.total += s_sum[i];
+  }
+  return s;
 }
 
 }  // namespace topkv_attend
