@@ -674,7 +674,7 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
  * descriptors, options, null pointers or a short or misaligned workspace,
  * TOPKV_ERR_UNSUPPORTED for head_dim above 1024, more than
  * TOPKV_MAX_BATCH_REQS requests, bt_stride * page_size of 2^30 or more,
- * num_reqs * bt_stride * page_size of 2^31 or more or 2^31 (token, head) rows, TOPKV_ERR_LAUNCH.  Does not synchronise and can be
+ * num_reqs * bt_stride * page_size of 2^31 or more or 2^30 (token, head) rows, TOPKV_ERR_LAUNCH.  Does not synchronise and can be
  * captured into a graph. */
 topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_attention_t* attn,
                                       int32_t num_reqs, const int32_t* seq_lens, const void* q, void* out,
@@ -683,7 +683,8 @@ topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_att
 /* Any number of new tokens per request (a prompt, a chunk of one, or the few
  * tokens of a draft): request r's are rows q_starts[r] .. q_starts[r + 1] - 1
  * of q, the last of them at position seq_lens[r] - 1.
- *   q_starts:  device int32[num_reqs + 1], ascending; clamped to [0, total_q]
+ *   q_starts:  device int32[num_reqs + 1], clamped to [0, total_q]; ascending,
+ *              else which rows are written is unspecified (none outside q's)
  *   total_q:   rows of q, out and lse; rows that belong to no request are
  *              left as they were
  * A token whose position would be negative (more new tokens than seq_lens[r])

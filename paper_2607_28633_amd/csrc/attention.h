@@ -26,12 +26,14 @@ struct Args {
   int64_t q_stride, out_stride;
   int32_t page_size, bt_stride, num_reqs, total_q;
   uint32_t page_mul, page_shift;   // position / page_size = position * page_mul >> page_shift, positions below 2^30
+  uint32_t group_mul, group_shift; // row / group likewise
   int32_t num_heads, kv_heads, group;
   int32_t head_dim, value_dim;
   int32_t window, sinks;
   float scale;                // scale * k_scale * log2(e): scores in powers of two
   float v_scale;
   int32_t dtype, kv_dtype;
+  bool out_wide;              // rows of out on 16-byte addresses
 };
 
 constexpr float kLn2 = 0.693147180559945309f;
@@ -69,6 +71,11 @@ __device__ __forceinline__ int32_t key_position(const Span& s, int32_t i) { retu
 // too large in 2^(30 + l), which no j below 2^30 can feel.
 __device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t j) {
   return (uint32_t)((uint64_t)j * a.page_mul >> a.page_shift);
+}
+
+// The new token that a row of a KV head's group belongs to.
+__device__ __forceinline__ int32_t token_of(const Args& a, int32_t row) {
+  return (int32_t)((uint64_t)(uint32_t)row * a.group_mul >> a.group_shift);
 }
 
 // Byte offset of position j's row from a.cache, or -1 when its page lies

@@ -114,6 +114,13 @@ topkv_status_t run_general(const Args& a, hipStream_t stream) {
   return hipGetLastError() == hipSuccess ? TOPKV_OK : TOPKV_ERR_LAUNCH;
 }
 
+void divider(int32_t d, uint32_t* mul, uint32_t* shift) {
+  int log2 = 0;
+  while ((int64_t)1 << log2 < d) ++log2;
+  *shift = 30 + log2;
+  *mul = (uint32_t)((((uint64_t)1 << *shift) + d - 1) / d);
+}
+
 // Checks of the view and options, and the part of Args that follows from them.
 topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32_t num_reqs, int32_t total_q, Args* a) {
   if (!v || !t) return TOPKV_ERR_INVALID_ARG;
@@ -139,7 +146,7 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
     return TOPKV_ERR_INVALID_ARG;
   if (num_reqs < 0 || total_q < 0) return TOPKV_ERR_INVALID_ARG;
   if (p.head_dim > 1024 || num_reqs > TOPKV_MAX_BATCH_REQS || (int64_t)v->bt_stride * p.page_size >= (1 << 30) ||
-      (int64_t)num_reqs * v->bt_stride * p.page_size > INT32_MAX || (int64_t)total_q * t->num_heads > INT32_MAX)
+      (int64_t)num_reqs * v->bt_stride * p.page_size > INT32_MAX || (int64_t)total_q * t->num_heads >= (1 << 30))
     return TOPKV_ERR_UNSUPPORTED;
   const int64_t elem = p.elem_bytes, plane = (int64_t)p.page_size * p.num_heads * p.head_dim * elem;
   const bool head_major = v->layout == TOPKV_LAYOUT_POOL_HEAD_MAJOR;
@@ -152,10 +159,8 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
   a->tables = v->block_tables;
   a->num_pages = p.num_pages;
   a->page_size = p.page_size;
-  int log2 = 0;
-  while ((int64_t)1 << log2 < p.page_size) ++log2;
-  a->page_shift = 30 + log2;
-  a->page_mul = (uint32_t)((((uint64_t)1 << a->page_shift) + p.page_size - 1) / p.page_size);
+  divider(p.page_size, &a->page_mul, &a->page_shift);
+  divider(t->num_heads / t->kv_heads, &a->group_mul, &a->group_shift);
   a->bt_stride = v->bt_stride;
   a->num_reqs = num_reqs;
   a->total_q = total_q;
@@ -200,8 +205,9 @@ topkv_status_t attend(const topkv_view_t* cache, const topkv_attention_t* attn, 
   a.q = q;
   a.out = out;
   a.lse = lse;
+  a.out_wide = reinterpret_cast<uintptr_t>(out) % 16 == 0 && a.out_stride % 8 == 0;
   if (decode && decode_takes(a) && aligned(a)) return run_decode(a, workspace, stream);
-  if (!decode && prompt_takes(a) && aligned(a)) return run_prompt(a, stream);
+  if (!decode && prompt_takes(a) && aligned(a)) return run_prompt(a, workspace, stream);
   return run_general(a, stream);
 }
 
@@ -213,7 +219,9 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
                                         int32_t total_q) {
   topkv_attend::Args a;
   if (topkv_attend::describe(cache, attn, num_reqs, total_q, &a) != TOPKV_OK) return -1;
-  return topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a) : 0;
+  const int64_t one = topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a) : 0;
+  const int64_t many = topkv_attend::prompt_takes(a) ? topkv_attend::prompt_workspace(a) : 0;
+  return one > many ? one : many;
 }
 
 topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_attention_t* attn, int32_t num_reqs,

@@ -39,7 +39,8 @@ struct Plan {
   int32_t shares;      // wanted; 0: one per request, whatever its length
   float* part;         // [2 * share + 1 for a request's first piece][kv head][row of the group][value_dim]
   float2v* part_ml;    // the same without value_dim: maximum and sum
-  int2* cut;           // [request]: pieces, share of the first
+  bool by_request;     // what `cut` is indexed by: requests, or shares where these are fewer
+  int4* cut;           // the request in pieces (of that number, or that starts in that share), its first share, how many (0: none)
 };
 
 struct Share {
@@ -59,11 +60,11 @@ __device__ Share find_share(const Args& a, int32_t shares, int32_t share) {
   __shared__ Share s_got;
   if (threadIdx.x == 0) s_got.request = -1;
   const auto tiles = [&](int32_t r) { return tiles_of(a, r); };
-  Scan n = scan_requests<kWaves>(a.num_reqs, tiles);
+  Scan<int32_t> n = scan_requests<int32_t, kWaves>(a.num_reqs, tiles);
   int32_t size = (n.total + shares - 1) / shares;
   size = size < kLeast ? kLeast : size;
   const int32_t first = share * size;
-  if (first >= n.base && first < n.base + n.mine) {
+  if (n.holds(first)) {
     s_got.request = n.find(first, tiles);
     s_got.base = n.base;
   }
@@ -106,7 +107,9 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   Share sh = {share, 0, 0, 0};
   int32_t tile_at = 0, tile_end = 1;                             // tiles of the batch; uncut: the request as one
   if constexpr (kCut) {
+    if (share >= plan.shares) return;
     sh = find_share(a, plan.shares, share);
+    if (!plan.by_request && sub == 0 && threadIdx.x == 0) plan.cut[share] = make_int4(0, 0, 0, 0);
     if (sh.request < 0) return;
     tile_at = share * sh.size;
     tile_end = tile_at + sh.size < sh.total ? tile_at + sh.size : sh.total;
@@ -126,8 +129,9 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
     whole = opens && to == tiles;
     begin = from * kTile;
     end = to * kTile < span.count ? to * kTile : span.count;
-    if (opens && sub == 0 && threadIdx.x == 0)
-      plan.cut[request] = make_int2((sh.base + tiles - 1) / sh.size - share + 1, share);
+    if (opens && (!whole || plan.by_request) && sub == 0 && threadIdx.x == 0)
+      plan.cut[plan.by_request ? request : share] =
+          make_int4(request, share, whole ? 0 : (sh.base + tiles - 1) / sh.size - share + 1, 0);
     tile_at = sh.base + to;
     sh.base += tiles;
   } else {
@@ -336,7 +340,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   }
 }
 
-// Requests in pieces: one workgroup per (request, query head, 64 elements).
+// Requests in pieces: one workgroup per (request or share, query head, 64 elements).
 // The pieces' weights first, then their sum with the pieces over the waves and
 // the elements over the lanes, so that no load waits for another.
 constexpr int kJoinWaves = 8;
@@ -344,20 +348,21 @@ constexpr int kJoinWaves = 8;
 template <int T>
 __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Args a, Plan plan) {
   __shared__ float s_weight[resident(128)], s_sum[kJoinWaves], s_part[kJoinWaves][64];
-  const int32_t r = blockIdx.x / a.num_heads, head = blockIdx.x - r * a.num_heads;
-  const int2 cut = plan.cut[r];
-  if (cut.x <= 1) return;
+  const int32_t entry = blockIdx.x / a.num_heads, head = blockIdx.x - entry * a.num_heads;
+  const int4 cut = plan.cut[entry];
+  const int32_t r = cut.x, share = cut.y, pieces = cut.z;
+  if (pieces == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t step = (int64_t)a.kv_heads * a.group;
-  const int64_t at = 2 * (int64_t)cut.y * step + head;            // piece k: slot 2 (first + k), the first one's next to it
+  const int64_t at = 2 * (int64_t)share * step + head;            // piece k: slot 2 (first + k), the first one's next to it
   const int32_t d = blockIdx.y * 64 + lane;
   float top = -INFINITY;                                         // every wave over all chunks
-  for (int32_t k = lane; k < cut.x; k += 64) top = fmaxf(top, plan.part_ml[at + (k ? 2 * k : 1) * step][0]);
+  for (int32_t k = lane; k < pieces; k += 64) top = fmaxf(top, plan.part_ml[at + (k ? 2 * k : 1) * step][0]);
 #pragma unroll
   for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
   const float base = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
-  for (int32_t k = threadIdx.x; k < cut.x; k += 64 * kJoinWaves) {
+  for (int32_t k = threadIdx.x; k < pieces; k += 64 * kJoinWaves) {
     const float2v ml = plan.part_ml[at + (k ? 2 * k : 1) * step];
     const float f = __builtin_amdgcn_exp2f(ml[0] - base);
     s_weight[k] = f;
@@ -372,7 +377,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Args
     const float* from = plan.part + at * a.value_dim + d;
     const int64_t row = step * a.value_dim;
 #pragma unroll 8
-    for (int32_t k = wave; k < cut.x; k += kJoinWaves) o = fmaf(s_weight[k], from[(k ? 2 * k : 1) * row], o);
+    for (int32_t k = wave; k < pieces; k += kJoinWaves) o = fmaf(s_weight[k], from[(k ? 2 * k : 1) * row], o);
   }
   s_part[wave][lane] = o;
   __syncthreads();
@@ -424,7 +429,7 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
   }
 #undef TOPKV_DECODE
   if (p.shares > 0)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)(a.num_reqs * a.num_heads), (unsigned)((a.value_dim + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, a, p);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)((p.by_request ? a.num_reqs : p.shares) * a.num_heads), (unsigned)((a.value_dim + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, a, p);
 }
 
 }  // namespace
@@ -435,14 +440,14 @@ bool decode_takes(const Args& a) {
   if (a.head_dim % 8 != 0 || (latent ? a.head_dim > 576 || a.value_dim > 512 : a.head_dim > 256)) return false;
   if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
   const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
-  return items * units(a) <= INT32_MAX && (int64_t)a.num_reqs * a.num_heads <= INT32_MAX;
+  return items * units(a) <= INT32_MAX && (int64_t)wanted_shares(a) * a.num_heads <= INT32_MAX;
 }
 
 int64_t decode_workspace(const Args& a) {
   const int32_t shares = wanted_shares(a);
   if (shares == 0) return 0;
   const int64_t rows = 2 * (int64_t)shares * a.kv_heads * a.group;
-  return up16(rows * a.value_dim * 4) + up16(rows * 8) + up16((int64_t)a.num_reqs * 8);
+  return up16(rows * a.value_dim * 4) + up16(rows * 8) + (int64_t)shares * 16;
 }
 
 topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream) {
@@ -455,7 +460,8 @@ topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream) {
     at += up16(rows * a.value_dim * 4);
     p.part_ml = reinterpret_cast<float2v*>(at);
     at += up16(rows * 8);
-    p.cut = reinterpret_cast<int2*>(at);
+    p.cut = reinterpret_cast<int4*>(at);
+    p.by_request = a.num_reqs <= p.shares;
   }
   if (a.kv_dtype == TOPKV_FP8_E4M3) {
     if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, p, stream);

@@ -128,33 +128,35 @@ __device__ __forceinline__ void wave_fence() {
 
 // Running sums of a weight over the requests, each thread of the workgroup
 // with a run of neighbours; find() is for the thread whose run holds an item.
+template <class I>
 struct Scan {
   int32_t lo, hi;      // the thread's requests
-  int32_t base, mine;  // weight before them and of them
-  int32_t total;
+  I base, mine;        // weight before them and of them
+  I total;
 
+  __device__ bool holds(I item) const { return item >= base && item < base + mine; }
   // The request that item number `item` belongs to; base becomes its first item.
-  template <class F> __device__ int32_t find(int32_t item, F weight) {
+  template <class F> __device__ int32_t find(I item, F weight) {
     int32_t r = lo;
-    for (int32_t w = weight(r); item >= base + w; w = weight(++r)) base += w;
+    for (I w = weight(r); item >= base + w && r + 1 < hi; w = weight(++r)) base += w;
     return r;
   }
 };
 
-template <int kWaves, class F>
-__device__ Scan scan_requests(int32_t num_reqs, F weight) {
-  __shared__ int32_t s_sum[kWaves];
+template <class I, int kWaves, class F>
+__device__ Scan<I> scan_requests(int32_t num_reqs, F weight) {
+  __shared__ I s_sum[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t per = (num_reqs + 64 * kWaves - 1) / (64 * kWaves);
-  Scan s;
+  Scan<I> s;
   s.lo = threadIdx.x * per;
   s.hi = s.lo + per < num_reqs ? s.lo + per : num_reqs;
   s.mine = 0;
   for (int32_t r = s.lo; r < s.hi; ++r) s.mine += weight(r);
-  int32_t inc = s.mine;
+  I inc = s.mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int32_t x = __shfl_up(inc, d, 64);
+    const I x = __shfl_up(inc, d, 64);
     if (lane >= d) inc += x;
   }
   if (lane == 63) s_sum[wave] = inc;

@@ -10,6 +10,12 @@
 // products is what has to hide behind the other wave of the SIMD.  While a
 // tile is multiplied the next one is on its way to registers and goes into the
 // other half of a double buffer: one barrier a tile.
+//
+// Many row tiles keep the GPU busy by themselves, the longest started first.
+// Few of them (a short chunk behind a long cache, one KV head) are cut along
+// the keys, like decode's requests: equal shares of the work, one for each
+// workgroup that fits the GPU at once, and a second kernel that joins the row
+// tiles that were cut.
 #include <type_traits>
 
 #include "attention_internal.h"
@@ -28,9 +34,41 @@ constexpr int kRows = kWaves * kWaveRows;
 // stay below 2^8, which either 16-bit type holds as exactly as those below 1, and most tiles need no rescaling.
 constexpr float kSlack = 8.f;
 
-__device__ __forceinline__ int32_t row_tiles(const Args& a, int32_t r) {
-  const int32_t s = clamped_start(a, r), e = clamped_start(a, r + 1);
-  return e > s ? (int32_t)(((int64_t)(e - s) * a.group + kRows - 1) / kRows) : 0;
+
+constexpr int resident(int KD) { return KD <= 64 ? 768 : KD <= 128 ? 512 : 256; }   // workgroups that 256 CUs hold at once
+constexpr int kLeast = 4;                // key tiles of a share, at least
+
+struct Plan {
+  int32_t most;        // row tiles that ascending q_starts can make
+  int32_t shares;      // wanted; 0: a workgroup per row tile
+  float* part;         // [2 * share + 1 for a row tile's first piece][kv head][kRows][head_dim]
+  float2v* part_ml;    // the same without head_dim: maximum and sum
+  int4* cut;           // [share]: request and first row of the row tile that starts in it and goes on, pieces (0: none)
+};
+
+struct Rows {          // one request's new tokens
+  int32_t first, count, shift;           // in q; shift: position of the first of them
+
+  __device__ int32_t tiles(const Args& a) const { return (int32_t)(((int64_t)count * a.group + kRows - 1) / kRows); }
+  // what the rows of row tile i see
+  __device__ Span span(const Args& a, int32_t i) const {
+    const int64_t rows = (int64_t)count * a.group, last = (int64_t)(i + 1) * kRows < rows ? (int64_t)(i + 1) * kRows : rows;
+    return key_span(a, shift + token_of(a, i * kRows), shift + token_of(a, (int32_t)last - 1));
+  }
+  // key tiles of the last row tile, at least 1: every row tile of the request counts as this many when work is shared out
+  __device__ int32_t depth(const Args& a) const {
+    const int32_t n = (span(a, tiles(a) - 1).count + kTile - 1) / kTile;
+    return n < 1 ? 1 : n;
+  }
+};
+
+__device__ __forceinline__ Rows rows_of(const Args& a, int32_t r) {
+  Rows w;
+  w.first = clamped_start(a, r);
+  const int32_t end = clamped_start(a, r + 1);
+  w.count = end > w.first ? end - w.first : 0;
+  w.shift = clamped_len(a, r) - w.count;
+  return w;
 }
 
 // Eight 16-bit values with infinities and NaN as zeros; *any is set where there were some.
@@ -46,8 +84,8 @@ __device__ __forceinline__ uint4v without_special(uint4v w, bool* any) {
   return w;
 }
 
-template <int T, bool kF8, int KD>
-__global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_prompt_kernel(Args a) {
+template <int T, bool kF8, int KD, bool kCut>
+__global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_prompt_kernel(Args a, Plan plan) {
   typedef typename Elem<T>::vec8 vec8;
   typedef typename Elem<T>::type elem;
   constexpr int NC = KD / 8;                                     // 16-byte chunks of a row in LDS
@@ -55,45 +93,97 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_promp
   constexpr int kHalf = kTile * KD * 2;                          // bytes of a tile's keys
   __shared__ __attribute__((aligned(16))) char s_tile[2][2 * kHalf];
   __shared__ int32_t s_special[2][kWaves];
-  __shared__ int32_t s_request, s_base;
+  __shared__ int32_t s_request;
+  __shared__ int64_t s_base;
+  __shared__ Rows s_rows;
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, half = lane >> 5;
 
-  // Which rows: eight row tiles side by side over the eight XCDs, a tile's KV heads one after the other on one XCD
-  // (whose L2 then sees whole rows of the cache, and neighbouring row tiles the same keys), the last, longest first.
-  const auto tiles = [&](int32_t r) { return row_tiles(a, r); };
-  Scan scan = scan_requests<kWaves>(a.num_reqs, tiles);
+  // Eight row tiles (or shares) side by side over the eight XCDs, their KV heads one after the other on one XCD (whose
+  // L2 then sees whole rows of the cache, and neighbouring row tiles the same keys).
   const int32_t eight = blockIdx.x / (8 * a.kv_heads), within = blockIdx.x - eight * 8 * a.kv_heads;
-  const int32_t item = scan.total - 1 - (eight * 8 + (within & 7)), kv_head = within >> 3;
-  if (item < 0) return;
-  if (item >= scan.base && item < scan.base + scan.mine) {
-    s_request = scan.find(item, tiles);
+  const int32_t number = eight * 8 + (within & 7), kv_head = within >> 3;
+  const auto weight = [&](int32_t r) -> int64_t {
+    const Rows w = rows_of(a, r);
+    const int32_t n = w.tiles(a);
+    return kCut && n > 0 ? (int64_t)n * w.depth(a) : n;
+  };
+  if (kCut && number >= plan.shares) return;
+  if (threadIdx.x == 0) s_request = -1;
+  Scan<int64_t> scan = scan_requests<int64_t, kWaves>(a.num_reqs, weight);
+  int64_t size = 1, at, upto;
+  if constexpr (kCut) {
+    size = (scan.total + plan.shares - 1) / plan.shares;
+    size = size < kLeast ? kLeast : size;
+    at = number * size;
+    upto = at + size < scan.total ? at + size : scan.total;
+    if (kv_head == 0 && threadIdx.x == 0) plan.cut[number] = make_int4(0, 0, 0, 0);
+  } else {
+    if (scan.total > plan.most) return;                          // q_starts do not ascend
+    at = scan.total - 1 - number;                                // the last, longest first
+    upto = at + 1;
+  }
+  if (at >= 0 && scan.holds(at)) {
+    s_request = scan.find(at, weight);
     s_base = scan.base;
+    s_rows = rows_of(a, s_request);
   }
   __syncthreads();
-  const int32_t request = __builtin_amdgcn_readfirstlane(s_request);
-  const int32_t first_row = (item - __builtin_amdgcn_readfirstlane(s_base)) * kRows;
+  int32_t request = __builtin_amdgcn_readfirstlane(s_request);
+  if (request < 0) return;
+  int64_t base = s_base;
+  Rows mine = s_rows;
 
-  const int32_t q_first = clamped_start(a, request), q_count = clamped_start(a, request + 1) - q_first;
-  const int64_t rows = (int64_t)q_count * a.group;
-  const int32_t shift = clamped_len(a, request) - q_count;       // position of the request's first new token
+  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
+  const int32_t chunks = a.head_dim / 8;
+  constexpr int kChunkBytes = kF8 ? 8 : 16;
+  typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
+  if (chunks < NC) {                                             // padding stays zero: loads leave it alone
+    for (int i = threadIdx.x; i < 2 * 2 * kHalf / 16; i += kThreads)
+      *reinterpret_cast<uint4v*>(&s_tile[0][0] + i * 16) = uint4v{0, 0, 0, 0};
+    __syncthreads();
+  }
+
+  while (at < upto) {
+  int32_t row_tile = (int32_t)(at - base);
+  int32_t key_from = 0, key_to = INT32_MAX;                      // key tiles of this piece
+  bool whole = true, opens = true;
+  if constexpr (kCut) {
+    const int32_t depth = mine.depth(a);
+    row_tile = (int32_t)((at - base) / depth);
+    const int32_t from = (int32_t)((at - base) - (int64_t)row_tile * depth);
+    const int32_t to = upto - at < depth - from ? from + (int32_t)(upto - at) : depth;
+    const int32_t have = (mine.span(a, row_tile).count + kTile - 1) / kTile;
+    key_from = (int32_t)((int64_t)have * from / depth);
+    key_to = (int32_t)((int64_t)have * to / depth);
+    opens = from == 0;
+    whole = opens && to == depth;
+    if (opens && !whole && kv_head == 0 && threadIdx.x == 0)
+      plan.cut[number] = make_int4(request, row_tile * kRows, (int32_t)((at + depth - 1) / size) - number + 1, 0);
+    at += to - from;
+  } else {
+    at = upto;
+  }
+  const int32_t first_row = row_tile * kRows;
+  const int32_t q_first = mine.first, shift = mine.shift;
+  const int64_t rows = (int64_t)mine.count * a.group;
   const int32_t last_row = (int32_t)(first_row + kRows < rows ? first_row + kRows : rows) - 1;
-  const Span span = key_span(a, shift + first_row / a.group, shift + last_row / a.group);
+  const Span span = mine.span(a, row_tile);
 
   // this lane's row, and the positions of the wave's rows
   const int32_t row = first_row + wave * kWaveRows + col;
   const bool real = row < rows;
-  const int32_t token = row / a.group, pos = real ? shift + token : -1;
+  const int32_t token = token_of(a, row), pos = real ? shift + token : -1;
   const int32_t head = kv_head * a.group + (row - token * a.group);
   const int32_t wave_row = first_row + wave * kWaveRows;
-  const int32_t wave_first = shift + wave_row / a.group;
+  const int32_t wave_first = shift + token_of(a, wave_row);
   const int32_t wave_last =
-      wave_row < rows ? shift + (int32_t)(wave_row + kWaveRows < rows ? wave_row + kWaveRows - 1 : rows - 1) / a.group : -1;
+      wave_row < rows ? shift + token_of(a, (int32_t)(wave_row + kWaveRows < rows ? wave_row + kWaveRows - 1 : rows - 1)) : -1;
 
   vec8 q[KD / 16];
   {
-    const char* at = static_cast<const char*>(a.q) + ((int64_t)(q_first + token) * a.q_stride + (int64_t)head * a.head_dim) * 2;
+    const char* from = static_cast<const char*>(a.q) + ((int64_t)(q_first + token) * a.q_stride + (int64_t)head * a.head_dim) * 2;
 #pragma unroll
     for (int s = 0; s < KD / 16; ++s) {
       const int d = s * 16 + half * 8;
@@ -102,23 +192,12 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_promp
         vec8 v;
       } u;
       u.w = uint4v{0, 0, 0, 0};
-      if (real && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(at + 2 * d);
+      if (real && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(from + 2 * d);
       q[s] = u.v;
     }
   }
 
   const int32_t* table = a.tables + (int64_t)request * a.bt_stride;
-  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
-  const int32_t chunks = a.head_dim / 8;
-  constexpr int kChunkBytes = kF8 ? 8 : 16;
-  typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
-
-  if (chunks < NC) {                                             // padding stays zero: loads leave it alone
-    for (int i = threadIdx.x; i < 2 * 2 * kHalf / 16; i += kThreads)
-      *reinterpret_cast<uint4v*>(&s_tile[0][0] + i * 16) = uint4v{0, 0, 0, 0};
-    __syncthreads();
-  }
-
   float16v acc[KD / 32];
 #pragma unroll
   for (int t = 0; t < KD / 32; ++t)
@@ -198,24 +277,27 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_promp
     return (k1 <= p0) & ((a.window == 0) | (k0 > p1 - a.window) | (k1 < a.sinks));
   };
 
-  const int32_t count = span.count;
-  const int32_t wg_first = shift + first_row / a.group, wg_last = shift + last_row / a.group;
-  int64_t off = locate(0, ask(0));
-  int32_t entry = ask(kTile);
+  const int32_t count = (int64_t)key_to * kTile < span.count ? key_to * kTile : span.count;   // end of the piece's keys
+  const int32_t begin = key_from * kTile;
+  const int32_t wg_first = shift + token_of(a, first_row), wg_last = shift + token_of(a, last_row);
+  int64_t off = locate(begin, ask(begin));
+  int32_t entry = ask(begin + kTile);
   uint64_t there = __ballot(off >= 0), there_next = 0;
-  fetch(0, off);
-  settle(0, there, !open(0, wg_first, wg_last));
+  if (begin < count) {
+    fetch(0, off);
+    settle(0, there, !open(begin, wg_first, wg_last));
+  }
   if constexpr (kF8) {
-    if (kTile < count) {
-      off = locate(kTile, entry);
-      entry = ask(2 * kTile);
+    if (begin + kTile < count) {
+      off = locate(begin + kTile, entry);
+      entry = ask(begin + 2 * kTile);
       there_next = __ballot(off >= 0);
       fetch(1, off);
     }
   }
   __syncthreads();
 
-  for (int32_t first = 0, buf = 0; first < count; first += kTile, buf ^= 1) {
+  for (int32_t first = begin, buf = 0; first < count; first += kTile, buf ^= 1) {
     const char* keys = s_tile[buf];
     const char* values = keys + kHalf;
     if constexpr (!kF8) {
@@ -318,7 +400,7 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_promp
 #pragma unroll
                   for (int i = 0; i < 4; ++i) {
                     const float f = Load<kF8 ? TOPKV_FP8_E4M3 : T>::at(v + (t * 32 + o * 8 + i) * (kF8 ? 1 : 2));
-                    acc[t][o * 4 + i] += seen & !(__builtin_fabsf(f) < INFINITY) ? f : 0.f;
+                    acc[t][o * 4 + i] += (seen & !(__builtin_fabsf(f) < INFINITY)) ? f : 0.f;
                   }
           }
         }
@@ -338,34 +420,139 @@ __global__ __launch_bounds__(kThreads, KD > 128 ? 1 : 2) void kv_attention_promp
   }
 
   l = sum_halves(l);
-  if (!real) return;
-  const float inv = l == 0.f ? 0.f : a.v_scale / l;
-  elem* out = static_cast<elem*>(a.out) + (int64_t)(q_first + token) * a.out_stride + (int64_t)head * a.value_dim;
+  if (!whole) {
+    if (real) {
+      const int64_t slot = ((2 * (int64_t)number + opens) * a.kv_heads + kv_head) * kRows + (row - first_row);
+      float* out = plan.part + slot * a.head_dim;
 #pragma unroll
-  for (int t = 0; t < KD / 32; ++t)
+      for (int t = 0; t < KD / 32; ++t)
 #pragma unroll
-    for (int o = 0; o < 4; ++o)
-      if (t * 32 + o * 8 < a.head_dim)
+        for (int o = 0; o < 4; ++o)
+          if (t * 32 + o * 8 < a.head_dim)
+            *reinterpret_cast<float4v*>(out + t * 32 + o * 8 + half * 4) =
+                float4v{acc[t][o * 4], acc[t][o * 4 + 1], acc[t][o * 4 + 2], acc[t][o * 4 + 3]};
+      if (half == 0) plan.part_ml[slot] = float2v{m, l};
+    }
+  } else {
+    const float inv = l == 0.f ? 0.f : a.v_scale / l;
+    elem* out = static_cast<elem*>(a.out) + (int64_t)(q_first + token) * a.out_stride + (int64_t)head * a.value_dim;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          out[t * 32 + o * 8 + half * 4 + i] = (elem)(l == 0.f ? 0.f : acc[t][o * 4 + i] * inv);
-  if (a.lse && half == 0)
-    a.lse[(int64_t)(q_first + token) * a.num_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    for (int t = 0; t < KD / 32; ++t)
+#pragma unroll
+      for (int o = 0; o < 4; o += 2) {
+        // 4 elements of chunk o and 4 of o + 1 a lane, the other 4 of each in the other half: exchanged, a lane has 8 of one
+        union {
+          elem e[8];
+          uint4v w;
+        } u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u.e[i] = (elem)(l == 0.f ? 0.f : acc[t][o * 4 + i] * inv);
+        const auto x = __builtin_amdgcn_permlane32_swap(u.w[0], u.w[2], false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(u.w[1], u.w[3], false, false);
+        u.w = uint4v{x[0], y[0], x[1], y[1]};
+        const int d = t * 32 + (o + half) * 8;
+        if (real && d < a.head_dim) {
+          if (a.out_wide) {
+            *reinterpret_cast<uint4v*>(out + d) = u.w;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[d + i] = u.e[i];
+          }
+        }
+      }
+    if (real && a.lse && half == 0)
+      a.lse[(int64_t)(q_first + token) * a.num_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+  if constexpr (kCut) {
+    // on to the next row tile, of a later request where this one's are done
+    if (at < upto && at == base + (int64_t)mine.tiles(a) * mine.depth(a)) {
+      base = at;
+      do mine = rows_of(a, ++request);
+      while (mine.count == 0 && request + 1 < a.num_reqs);
+    }
+  }
+  }
 }
+
+// Row tiles in pieces: a workgroup for 16 rows of (share that one starts in,
+// KV head), a wave for 4 of them.
+template <int T>
+__global__ __launch_bounds__(kThreads) void kv_attention_prompt_join_kernel(Args a, Plan plan) {
+  const int32_t share = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - share * a.kv_heads;
+  const int4 cut = plan.cut[share];
+  if (cut.z == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Rows mine = rows_of(a, cut.x);
+  const int64_t step = (int64_t)a.kv_heads * kRows;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int32_t in_tile = blockIdx.y * 16 + wave * 4 + i, row = cut.y + in_tile;
+    if (row >= (int64_t)mine.count * a.group) return;
+    const int32_t token = token_of(a, row), head = kv_head * a.group + (row - token * a.group);
+    const int64_t slot = (2 * (int64_t)share * a.kv_heads + kv_head) * kRows + in_tile;   // piece k: 2 k steps on, the first 1
+    float top = -INFINITY;
+    for (int32_t k = lane; k < cut.z; k += 64) top = fmaxf(top, plan.part_ml[slot + (k ? 2 * k : 1) * step][0]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int32_t k = 0; k < cut.z; ++k) {
+      const int64_t s = slot + (k ? 2 * k : 1) * step;
+      const float2v ml = plan.part_ml[s];
+      const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+      sum = fmaf(f, ml[1], sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e * 64 + lane < a.head_dim) o[e] = fmaf(f, plan.part[s * a.head_dim + e * 64 + lane], o[e]);
+    }
+    const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
+    typename Elem<T>::type* out = static_cast<typename Elem<T>::type*>(a.out) + (int64_t)(mine.first + token) * a.out_stride +
+                                  (int64_t)head * a.value_dim;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e * 64 + lane < a.head_dim) out[e * 64 + lane] = (typename Elem<T>::type)(sum == 0.f ? 0.f : o[e] * inv);
+    if (a.lse && lane == 0)
+      a.lse[(int64_t)(mine.first + token) * a.num_heads + head] =
+          sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// Row tiles that any division of the rows among the requests can make, and that every one makes.
+int64_t most_tiles(const Args& a) { return (int64_t)a.total_q * a.group / kRows + a.num_reqs; }
+int64_t least_tiles(const Args& a) { return ((int64_t)a.total_q * a.group + kRows - 1) / kRows; }
+
+// Shares of the work, 0 where the row tiles are enough: twice as many as fit the GPU at once, so that the last of them
+// leave little of it idle; or where no row can see more keys than a share should have.
+int32_t wanted_shares(const Args& a) {
+  const int64_t fit = resident(a.head_dim), seen = (int64_t)a.bt_stride * a.page_size;
+  const int64_t most = a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
+  if (least_tiles(a) * a.kv_heads >= 2 * fit || most <= 2 * kLeast * kTile) return 0;
+  const int32_t n = (int32_t)(fit / a.kv_heads);
+  return n < 1 ? 1 : n;
+}
+
+int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 
 template <int T, bool kF8>
-void launch(const Args& a, int64_t items, hipStream_t stream) {
+void launch(const Args& a, const Plan& p, hipStream_t stream) {
+  const int64_t items = p.shares > 0 ? p.shares : p.most;
   const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.kv_heads)), block(kThreads);
-  if (a.head_dim <= 64)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, 64>), grid, block, 0, stream, a);
-  else if (a.head_dim <= 128)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, 128>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, 256>), grid, block, 0, stream, a);
+#define TOPKV_PROMPT(KD)                                                                                                 \
+  do {                                                                                                                   \
+    if (p.shares > 0)                                                                                                    \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, KD, true>), grid, block, 0, stream, a, p);   \
+    else                                                                                                                 \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, KD, false>), grid, block, 0, stream, a, p);  \
+  } while (0)
+  if (a.head_dim <= 64) TOPKV_PROMPT(64);
+  else if (a.head_dim <= 128) TOPKV_PROMPT(128);
+  else TOPKV_PROMPT(256);
+#undef TOPKV_PROMPT
+  if (p.shares > 0)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_join_kernel<T>), dim3((unsigned)(p.shares * a.kv_heads), kRows / 16),
+                       block, 0, stream, a, p);
 }
-
-// Row tiles that any division of the rows among the requests can make.
-int64_t most_tiles(const Args& a) { return (int64_t)a.total_q * a.group / kRows + a.num_reqs; }
 
 }  // namespace
 
@@ -373,18 +560,35 @@ bool prompt_takes(const Args& a) {
   const int64_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
   if (a.value_bytes == 0 || a.head_dim % 8 != 0 || a.head_dim > 256) return false;
   if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
-  return (most_tiles(a) + 8) * a.kv_heads <= INT32_MAX;
+  const int64_t items = most_tiles(a) > wanted_shares(a) ? most_tiles(a) : wanted_shares(a);
+  return (items + 8) * a.kv_heads <= INT32_MAX;
 }
 
-topkv_status_t run_prompt(const Args& a, hipStream_t stream) {
-  const int64_t items = most_tiles(a);
+int64_t prompt_workspace(const Args& a) {
+  const int64_t shares = ((int64_t)wanted_shares(a) + 7) / 8 * 8, rows = 2 * shares * a.kv_heads * kRows;
+  return up16(rows * a.head_dim * 4) + up16(rows * 8) + shares * 16;
+}
+
+topkv_status_t run_prompt(const Args& a, void* workspace, hipStream_t stream) {
+  Plan p = {};
+  p.most = (int32_t)most_tiles(a);
+  p.shares = wanted_shares(a);
+  if (p.shares > 0) {
+    const int64_t shares = ((int64_t)p.shares + 7) / 8 * 8, rows = 2 * shares * a.kv_heads * kRows;
+    char* at = static_cast<char*>(workspace);
+    p.part = reinterpret_cast<float*>(at);
+    at += up16(rows * a.head_dim * 4);
+    p.part_ml = reinterpret_cast<float2v*>(at);
+    at += up16(rows * 8);
+    p.cut = reinterpret_cast<int4*>(at);
+  }
   if (a.kv_dtype == TOPKV_FP8_E4M3) {
-    if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, items, stream);
-    else launch<TOPKV_FP16, true>(a, items, stream);
+    if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, p, stream);
+    else launch<TOPKV_FP16, true>(a, p, stream);
   } else if (a.dtype == TOPKV_BF16) {
-    launch<TOPKV_BF16, false>(a, items, stream);
+    launch<TOPKV_BF16, false>(a, p, stream);
   } else {
-    launch<TOPKV_FP16, false>(a, items, stream);
+    launch<TOPKV_FP16, false>(a, p, stream);
   }
   return hipGetLastError() == hipSuccess ? TOPKV_OK : TOPKV_ERR_LAUNCH;
 }
