@@ -17,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = [os.path.join(PKG, "csrc", n) for n in ("topkv.hip", "check.hip", "kvcache1.hip", "dma.hip", "reshard.hip",
                                                   "state.hip", "pages.hip", "attention.hip",
-                                                  "attention_decode.hip", "attention_prompt.hip")]
+                                                  "attention_decode.hip", "attention_latent.hip", "attention_prompt.hip")]
 CEILING_SOURCES = [os.path.join(PKG, "csrc", "ceiling.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libtopkv.so")

@@ -207,6 +207,7 @@ topkv_status_t attend(const topkv_view_t* cache, const topkv_attention_t* attn, 
   a.lse = lse;
   a.out_wide = reinterpret_cast<uintptr_t>(out) % 16 == 0 && a.out_stride % 8 == 0;
   if (decode && decode_takes(a) && aligned(a)) return run_decode(a, workspace, stream);
+  if (decode && latent_takes(a) && aligned(a)) return run_latent(a, workspace, stream);
   if (!decode && prompt_takes(a) && aligned(a)) return run_prompt(a, workspace, stream);
   return run_general(a, stream);
 }
@@ -219,7 +220,9 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
                                         int32_t total_q) {
   topkv_attend::Args a;
   if (topkv_attend::describe(cache, attn, num_reqs, total_q, &a) != TOPKV_OK) return -1;
-  const int64_t one = topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a) : 0;
+  const int64_t one = topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a)
+                      : topkv_attend::latent_takes(a) ? topkv_attend::latent_workspace(a)
+                                                      : 0;
   const int64_t many = topkv_attend::prompt_takes(a) ? topkv_attend::prompt_workspace(a) : 0;
   return one > many ? one : many;
 }

@@ -15,7 +15,7 @@
 // results in 32 bits.  The cut follows the lengths on the device, not the
 // width of the tables.
 #include "attention_internal.h"
-#include "attention_mfma.h"
+#include "attention_share.h"
 
 namespace topkv_attend {
 
@@ -23,57 +23,13 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kTile = 32;                // keys of one wave's tile
 constexpr int kRows = 16;                // query rows of a workgroup
-constexpr int kStep = kTile * kWaves;    // keys of the workgroup's tiles
-
-constexpr int kLeast = 8;                // tiles of a share, at least: smaller pieces cost more to join than they save
-constexpr int kSingle = 512;             // longest visible length that is never cut (one launch, no join)
+constexpr int kStep = kTile * kWaves;    // keys of the waves' tiles together
 
 // Shares, by the key width: as many workgroups as 256 CUs hold at once by their LDS (64 KiB at 128 elements, 128 KiB
 // at 256).  131072 tokens, 8 heads of 128: 512 shares 108 us, 768 114, 1024 113, 2048 121; heads of 64, of which four
 // workgroups fit a CU, 512 118 us, 768 123, 1024 131.
 constexpr int resident(int KD) { return KD <= 128 ? 512 : 256; }
-
-struct Plan {
-  int32_t shares;      // wanted; 0: one per request, whatever its length
-  float* part;         // [2 * share + 1 for a request's first piece][kv head][row of the group][value_dim]
-  float2v* part_ml;    // the same without value_dim: maximum and sum
-  bool by_request;     // what `cut` is indexed by: requests, or shares where these are fewer
-  int4* cut;           // the request in pieces (of that number, or that starts in that share), its first share, how many (0: none)
-};
-
-struct Share {
-  int32_t request;     // of the first tile; -1: the share is empty
-  int32_t base;        // number of that request's first tile
-  int32_t size;        // tiles of a share
-  int32_t total;       // tiles of the batch
-};
-
-// Every request has at least one tile, so that those of no tokens are written too.
-__device__ __forceinline__ int32_t tiles_of(const Args& a, int32_t r) {
-  const int32_t p = clamped_len(a, r) - 1, n = key_span(a, p, p).count;
-  return n < 1 ? 1 : (n + kTile - 1) / kTile;
-}
-
-__device__ Share find_share(const Args& a, int32_t shares, int32_t share) {
-  __shared__ Share s_got;
-  if (threadIdx.x == 0) s_got.request = -1;
-  const auto tiles = [&](int32_t r) { return tiles_of(a, r); };
-  Scan<int32_t> n = scan_requests<int32_t, kWaves>(a.num_reqs, tiles);
-  int32_t size = (n.total + shares - 1) / shares;
-  size = size < kLeast ? kLeast : size;
-  const int32_t first = share * size;
-  if (n.holds(first)) {
-    s_got.request = n.find(first, tiles);
-    s_got.base = n.base;
-  }
-  __syncthreads();
-  Share got = s_got;
-  got.size = size;
-  got.total = n.total;
-  return got;
-}
 
 // KD, VD: key and value elements of a row, padded; kLatent: the value is the
 // key row's front.  T: the inputs' type; kF8: the cache holds e4m3.
@@ -89,8 +45,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   __shared__ __attribute__((aligned(16))) char s_tile[kWaves * kWaveBytes];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = lane & 15, quad = lane >> 4;
+  const int wave = threadIdx.x >> 6;
   const int32_t groups = (a.group + kRows - 1) / kRows;
   // Eight items side by side over the eight XCDs, an item's KV heads one after the other on one XCD: with the
   // heads side by side each XCD would read a narrow column of the cache through a few channels of its L2.
@@ -108,7 +63,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   int32_t tile_at = 0, tile_end = 1;                             // tiles of the batch; uncut: the request as one
   if constexpr (kCut) {
     if (share >= plan.shares) return;
-    sh = find_share(a, plan.shares, share);
+    sh = find_share<kWaves>(a, plan.shares, share);
     if (!plan.by_request && sub == 0 && threadIdx.x == 0) plan.cut[share] = make_int4(0, 0, 0, 0);
     if (sh.request < 0) return;
     tile_at = share * sh.size;
@@ -118,6 +73,9 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   }
 
   for (int32_t request = sh.request; tile_at < tile_end; ++request) {
+  int lane = threadIdx.x & 63;
+  if constexpr (kCut) asm volatile("" : "+v"(lane));             // addresses made from it stay in the loop: registers
+  const int row = lane & 15, quad = lane >> 4;
   const int32_t pos = clamped_len(a, request) - 1;
   const Span span = key_span(a, pos, pos);
   int32_t begin = 0, end = span.count;
@@ -340,72 +298,9 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
   }
 }
 
-// Requests in pieces: one workgroup per (request or share, query head, 64 elements).
-// The pieces' weights first, then their sum with the pieces over the waves and
-// the elements over the lanes, so that no load waits for another.
-constexpr int kJoinWaves = 8;
-
-template <int T>
-__global__ __launch_bounds__(64 * kJoinWaves) void kv_attention_join_kernel(Args a, Plan plan) {
-  __shared__ float s_weight[resident(128)], s_sum[kJoinWaves], s_part[kJoinWaves][64];
-  const int32_t entry = blockIdx.x / a.num_heads, head = blockIdx.x - entry * a.num_heads;
-  const int4 cut = plan.cut[entry];
-  const int32_t r = cut.x, share = cut.y, pieces = cut.z;
-  if (pieces == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t step = (int64_t)a.kv_heads * a.group;
-  const int64_t at = 2 * (int64_t)share * step + head;            // piece k: slot 2 (first + k), the first one's next to it
-  const int32_t d = blockIdx.y * 64 + lane;
-  float top = -INFINITY;                                         // every wave over all chunks
-  for (int32_t k = lane; k < pieces; k += 64) top = fmaxf(top, plan.part_ml[at + (k ? 2 * k : 1) * step][0]);
-#pragma unroll
-  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-  for (int32_t k = threadIdx.x; k < pieces; k += 64 * kJoinWaves) {
-    const float2v ml = plan.part_ml[at + (k ? 2 * k : 1) * step];
-    const float f = __builtin_amdgcn_exp2f(ml[0] - base);
-    s_weight[k] = f;
-    sum += f * ml[1];
-  }
-#pragma unroll
-  for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i, 64);
-  if (lane == 0) s_sum[wave] = sum;
-  __syncthreads();
-  float o = 0.f;
-  if (d < a.value_dim) {
-    const float* from = plan.part + at * a.value_dim + d;
-    const int64_t row = step * a.value_dim;
-#pragma unroll 8
-    for (int32_t k = wave; k < pieces; k += kJoinWaves) o = fmaf(s_weight[k], from[(k ? 2 * k : 1) * row], o);
-  }
-  s_part[wave][lane] = o;
-  __syncthreads();
-  if (wave > 0) return;
-  sum = 0.f;
-  o = 0.f;
-  for (int w = 0; w < kJoinWaves; ++w) {
-    sum += s_sum[w];
-    o += s_part[w][lane];
-  }
-  if (d < a.value_dim)
-    static_cast<typename Elem<T>::type*>(a.out)[(int64_t)r * a.out_stride + (int64_t)head * a.value_dim + d] =
-        (typename Elem<T>::type)(sum == 0.f ? 0.f : o * (a.v_scale / sum));
-  if (a.lse && d == 0)
-    a.lse[(int64_t)r * a.num_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
-}
-
 int32_t units(const Args& a) { return a.kv_heads * ((a.group + kRows - 1) / kRows); }
 
-int32_t wanted_shares(const Args& a) {
-  const int64_t seen = (int64_t)a.bt_stride * a.page_size;
-  const int64_t most = a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
-  if (most <= kSingle) return 0;
-  const int32_t n = resident(a.head_dim) / units(a);
-  return n < 1 ? 1 : n;
-}
-
-int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
+int32_t wanted_shares(const Args& a) { return shares_for(a, resident(a.head_dim), units(a)); }
 
 template <int T, bool kF8>
 void launch(const Args& a, const Plan& p, hipStream_t stream) {
@@ -419,50 +314,27 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
     else                                                                                                                     \
       hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_decode_kernel<T, kF8, KD, VD, LATENT, false>), grid, block, 0, stream, a, p); \
   } while (0)
-  if (latent) {
-    if (a.head_dim <= 128) TOPKV_DECODE(128, 128, true);
-    else TOPKV_DECODE(576, 512, true);
-  } else {
-    if (a.head_dim <= 64) TOPKV_DECODE(64, 64, false);
-    else if (a.head_dim <= 128) TOPKV_DECODE(128, 128, false);
-    else TOPKV_DECODE(256, 256, false);
-  }
+  if (latent) TOPKV_DECODE(128, 128, true);
+  else if (a.head_dim <= 64) TOPKV_DECODE(64, 64, false);
+  else if (a.head_dim <= 128) TOPKV_DECODE(128, 128, false);
+  else TOPKV_DECODE(256, 256, false);
 #undef TOPKV_DECODE
-  if (p.shares > 0)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<T>), dim3((unsigned)((p.by_request ? a.num_reqs : p.shares) * a.num_heads), (unsigned)((a.value_dim + 63) / 64)), dim3(64 * kJoinWaves), 0, stream, a, p);
+  launch_join(a, p, stream);
 }
 
 }  // namespace
 
 bool decode_takes(const Args& a) {
-  const int64_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
   const bool latent = a.value_bytes == 0;
-  if (a.head_dim % 8 != 0 || (latent ? a.head_dim > 576 || a.value_dim > 512 : a.head_dim > 256)) return false;
-  if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
+  if (!rows_aligned(a) || a.head_dim > (latent ? 128 : 256)) return false;
   const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
   return items * units(a) <= INT32_MAX && (int64_t)wanted_shares(a) * a.num_heads <= INT32_MAX;
 }
 
-int64_t decode_workspace(const Args& a) {
-  const int32_t shares = wanted_shares(a);
-  if (shares == 0) return 0;
-  const int64_t rows = 2 * (int64_t)shares * a.kv_heads * a.group;
-  return up16(rows * a.value_dim * 4) + up16(rows * 8) + (int64_t)shares * 16;
-}
+int64_t decode_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }
 
 topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream) {
-  Plan p = {};
-  p.shares = wanted_shares(a);
-  if (p.shares > 0) {
-    const int64_t rows = 2 * (int64_t)p.shares * a.kv_heads * a.group;
-    char* at = static_cast<char*>(workspace);
-    p.part = reinterpret_cast<float*>(at);
-    at += up16(rows * a.value_dim * 4);
-    p.part_ml = reinterpret_cast<float2v*>(at);
-    at += up16(rows * 8);
-    p.cut = reinterpret_cast<int4*>(at);
-    p.by_request = a.num_reqs <= p.shares;
-  }
+  const Plan p = make_plan(a, wanted_shares(a), workspace);
   if (a.kv_dtype == TOPKV_FP8_E4M3) {
     if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, p, stream);
     else launch<TOPKV_FP16, true>(a, p, stream);

@@ -12,6 +12,9 @@ __attribute__((visibility("hidden"))) bool decode_takes(const Args& a);
 __attribute__((visibility("hidden"))) int64_t decode_workspace(const Args& a);
 __attribute__((visibility("hidden"))) topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream);
 
+__attribute__((visibility("hidden"))) bool latent_takes(const Args& a);
+__attribute__((visibility("hidden"))) int64_t latent_workspace(const Args& a);
+__attribute__((visibility("hidden"))) topkv_status_t run_latent(const Args& a, void* workspace, hipStream_t stream);
 __attribute__((visibility("hidden"))) bool prompt_takes(const Args& a);
 __attribute__((visibility("hidden"))) int64_t prompt_workspace(const Args& a);
 __attribute__((visibility("hidden"))) topkv_status_t run_prompt(const Args& a, void* workspace, hipStream_t stream);

@@ -1,0 +1,364 @@
+// attention_latent.hip - one new token per request over a latent cache
+// (planes = 1, rows of up to 576 elements whose front is also the value) on
+// the matrix units.
+//
+// All query heads share one latent row, so a workgroup takes up to 64 of them
+// and the row is read from memory once for all: 2 * 64 * (576 + 512) flops
+// for 1152 bytes, still less than the matrix units do in the time the bytes
+// take.  The output, 64 rows of 512, is too much for one wave: the eight waves
+// of a workgroup share a tile of 32 keys.  For the scores a wave takes 16 keys
+// and 16 rows, for the output 64 elements of all rows; in between the weights
+// go through LDS.  Three tiles are in LDS, one in use and two on their way
+// straight from memory, which is what keeps the bytes coming: a CU holds one
+// workgroup.  Three barriers a tile cost little against the tile's bytes.
+#include <type_traits>
+
+#include "attention_internal.h"
+#include "attention_share.h"
+
+namespace topkv_attend {
+
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int KD = 576, VD = 512;        // elements of a row and of its value, padded
+constexpr int NC = KD / 8;               // 16-byte chunks of a row in LDS
+constexpr int kTileBytes = kTile * KD * 2;
+constexpr int kPieces = kTileBytes / 1024;               // wave-wide loads of a tile
+constexpr int kLoads = (kPieces + kWaves - 1) / kWaves;  // of a wave
+constexpr int kBuffers = 3;
+constexpr int kResident = 256;           // workgroups that 256 CUs hold at once
+constexpr float kSlack = 8.f;            // see attention_prompt.hip
+
+template <int T, bool kF8, int RB, bool kCut>
+__global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a, Plan plan) {
+  typedef typename Elem<T>::vec8 vec8;
+  typedef typename Elem<T>::type elem;
+  constexpr int kRows = 16 * RB;
+  __shared__ __attribute__((aligned(16))) char s_tile[kBuffers][kTileBytes];
+  __shared__ __attribute__((aligned(16))) elem s_weight[kRows][kTile];
+  __shared__ float s_top[2][kRows], s_sum[2][kRows];
+
+  const int wave = threadIdx.x >> 6;
+  const int key_half = wave & 1, row_block = wave >> 1;          // the wave's scores; none where row_block >= RB
+  const int32_t groups = (a.group + kRows - 1) / kRows;
+  const int32_t units = a.kv_heads * groups, eight = blockIdx.x / (8 * units), within = blockIdx.x - eight * 8 * units;
+  const int32_t share = eight * 8 + (within & 7), sub = within >> 3;   // over the XCDs as in attention_decode.hip
+  const int32_t kv_head = sub % a.kv_heads, first_row = sub / a.kv_heads * kRows;
+  const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
+  const int32_t chunks = a.head_dim / 8;
+  constexpr int kChunkBytes = kF8 ? 8 : 16;
+
+  Share sh = {share, 0, 0, 0};
+  int32_t tile_at = 0, tile_end = 1;
+  if constexpr (kCut) {
+    if (share >= plan.shares) return;
+    sh = find_share<kWaves>(a, plan.shares, share);
+    if (!plan.by_request && sub == 0 && threadIdx.x == 0) plan.cut[share] = make_int4(0, 0, 0, 0);
+    if (sh.request < 0) return;
+    tile_at = share * sh.size;
+    tile_end = tile_at + sh.size < sh.total ? tile_at + sh.size : sh.total;
+  } else {
+    if (share >= a.num_reqs) return;
+  }
+  if (chunks < NC) {                                             // padding stays zero: loads leave it alone
+    for (int i = threadIdx.x; i < kBuffers * kTileBytes / 16; i += kThreads)
+      *reinterpret_cast<uint4v*>(&s_tile[0][0] + i * 16) = uint4v{0, 0, 0, 0};
+    __syncthreads();
+  }
+
+  for (int32_t request = sh.request; tile_at < tile_end; ++request) {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));                                 // addresses made from it stay in the loop: registers
+  const int row = lane & 15, quad = lane >> 4;
+  const int32_t pos = clamped_len(a, request) - 1;
+  const Span span = key_span(a, pos, pos);
+  int32_t begin = 0, end = span.count;
+  bool whole = true, opens = false;
+  if constexpr (kCut) {
+    const int32_t tiles = span.count < 1 ? 1 : (span.count + kTile - 1) / kTile, from = tile_at - sh.base;
+    const int32_t to = tile_end - sh.base < tiles ? tile_end - sh.base : tiles;
+    opens = from == 0;
+    whole = opens && to == tiles;
+    begin = from * kTile;
+    end = to * kTile < span.count ? to * kTile : span.count;
+    if (opens && (!whole || plan.by_request) && sub == 0 && threadIdx.x == 0)
+      plan.cut[plan.by_request ? request : share] =
+          make_int4(request, share, whole ? 0 : (sh.base + tiles - 1) / sh.size - share + 1, 0);
+    tile_at = sh.base + to;
+    sh.base += tiles;
+  } else {
+    tile_at = tile_end;
+  }
+
+  const int32_t* table = a.tables + (int64_t)request * a.bt_stride;
+  const auto ask = [&](int32_t first) -> int32_t {
+    const int32_t v = first + (lane & 31);
+    return v < end ? table[page_of(a, (uint32_t)key_position(span, v))] : -1;
+  };
+  const auto locate = [&](int32_t first, int32_t entry) -> int64_t {
+    const int32_t v = first + (lane & 31);
+    if (v >= end || entry < 0 || entry >= a.num_pages) return -1;
+    const uint32_t j = (uint32_t)key_position(span, v);
+    return (int64_t)entry * a.page_bytes + (int64_t)(j - page_of(a, j) * (uint32_t)a.page_size) * a.slot_bytes;
+  };
+  // load i of the wave: 64 places of 16 bytes of the tile
+  uint2v raw[kF8 ? kLoads : 1];
+  const auto fetch = [&](int buf, int64_t off) {
+    const int lo = off < 0 ? 0 : (int)(uint32_t)off, hi = off < 0 ? 0 : (int)(off >> 32);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int piece = i * kWaves + wave;
+      if (piece < kPieces) {
+        const int place = piece * 64 + lane, r = place / NC, c = (place - r * NC) ^ swizzle<NC>(r);
+        const char* from =
+            cache + (int64_t)((uint64_t)(uint32_t)__shfl(hi, r, 64) << 32 | (uint32_t)__shfl(lo, r, 64)) + c * kChunkBytes;
+        if (c < chunks) {
+          if constexpr (kF8) raw[i] = *reinterpret_cast<const uint2v*>(from);
+          else load_to_lds(s_tile[buf] + piece * 1024, from);
+        }
+      }
+    }
+  };
+  // rows without a key as zeros, whatever their place holds; an 8-bit cache is widened on the way
+  const auto settle = [&](int buf, uint32_t there) {
+    if (!kF8 && there == ~0u) return;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int piece = i * kWaves + wave;
+      if (piece < kPieces) {
+        const int place = piece * 64 + lane, r = place / NC, c = (place - r * NC) ^ swizzle<NC>(r);
+        const bool is = there >> r & 1;
+        uint4v* to = reinterpret_cast<uint4v*>(s_tile[buf] + place * 16);
+        if (c < chunks) {
+          if constexpr (kF8) *to = is ? widen<T>(raw[i]) : uint4v{0, 0, 0, 0};
+          else if (!is) *to = uint4v{0, 0, 0, 0};
+        }
+      }
+    }
+  };
+
+  // tiles i, i + 1, i + 2: which keys are there
+  int32_t entry = ask(begin);
+  int64_t off = locate(begin, entry);
+  entry = ask(begin + kTile);
+  uint32_t there = (uint32_t)__ballot(off >= 0), there1 = 0, there2 = 0;
+  if (begin < end) fetch(0, off);
+  if constexpr (kF8) {
+    if (begin < end) settle(0, there);
+  }
+  off = locate(begin + kTile, entry);
+  entry = ask(begin + 2 * kTile);
+  there1 = (uint32_t)__ballot(off >= 0);
+  if (begin + kTile < end) fetch(1, off);
+
+  vec8 q[KD / 32];
+  {
+    const int32_t h = first_row + row_block * 16 + row;
+    const char* from =
+        static_cast<const char*>(a.q) + ((int64_t)request * a.q_stride + (int64_t)(kv_head * a.group + h) * a.head_dim) * 2;
+#pragma unroll
+    for (int s = 0; s < KD / 32; ++s) {
+      const int d = s * 32 + quad * 8;
+      union {
+        uint4v w;
+        vec8 v;
+      } u;
+      u.w = uint4v{0, 0, 0, 0};
+      if (row_block < RB && h < a.group && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(from + 2 * d);
+      q[s] = u.v;
+    }
+  }
+  float4v acc[RB][4];
+  float m[RB], l = 0.f;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    m[b] = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[b][t] = float4v{0.f, 0.f, 0.f, 0.f};
+  }
+
+  int buf = 0;
+  for (int32_t first = begin; first < end; first += kTile) {
+    const int next = buf + 1 < kBuffers ? buf + 1 : 0, last = next + 1 < kBuffers ? next + 1 : 0;
+    if constexpr (!kF8) {
+      // this wave's part of the tile has landed when no more than the next tile's loads (4 at least) are under way
+      // (narrower rows: some of a tile's loads may have no lane to them and are never issued)
+      if (first + kTile < end && chunks == NC) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      else wait_loads();
+      settle(buf, there);
+    }
+    __syncthreads();                                             // the tile is whole; the one before it is done with
+    if constexpr (kF8) {
+      if (first + kTile < end) settle(next, there1);
+    }
+    off = locate(first + 2 * kTile, entry);
+    there2 = (uint32_t)__ballot(off >= 0);
+    if (first + 2 * kTile < end) {
+      entry = ask(first + 3 * kTile);
+      fetch(last, off);
+    }
+    const char* tile = s_tile[buf];
+    int here = lane;
+    asm volatile("" : "+v"(here));                               // and these in the tile's loop
+    const int row = here & 15, quad = here >> 4;
+    float4v x = {0.f, 0.f, 0.f, 0.f};
+    if (row_block < RB) {
+      const int r = key_half * 16 + row;
+#pragma unroll
+      for (int s = 0; s < KD / 32; ++s) {
+        const vec8 k = *reinterpret_cast<const vec8*>(tile + (r * NC + ((s * 4 + quad) ^ swizzle<NC>(r))) * 16);
+        x = Elem<T>::mfma16(k, q[s], x);
+      }
+      if (there != ~0u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(there >> (key_half * 16 + quad * 4 + i) & 1)) x[i] = -INFINITY;
+      }
+      const float top = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale;
+      if (quad == 0) s_top[key_half][row_block * 16 + row] = top;
+    }
+    __syncthreads();
+    float fall_mine = 1.f, base_mine = 0.f;
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {                               // every wave keeps every row's maximum
+      const float top = fmaxf(s_top[0][b * 16 + row], s_top[1][b * 16 + row]);
+      float fall = 1.f;
+      if (__any(top > m[b] + kSlack)) {
+        const float up = fmaxf(m[b], top);
+        fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
+        m[b] = up;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[b][t] *= fall;
+      }
+      if (b == row_block) {
+        fall_mine = fall;
+        base_mine = m[b] == -INFINITY ? 0.f : m[b];
+      }
+    }
+    if (row_block < RB) {
+      l *= fall_mine;
+      union {
+        elem e[4];
+        uint2v w;
+      } u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base_mine));
+        l += w;
+        u.e[i] = (elem)w;                                        // rounded for the matrix units, its sum is not
+      }
+      *reinterpret_cast<uint2v*>(&s_weight[row_block * 16 + row][key_half * 16 + quad * 4]) = u.w;
+    }
+    __syncthreads();
+    vec8 p[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) p[b] = *reinterpret_cast<const vec8*>(&s_weight[b * 16 + row][quad * 8]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {                                // 16 elements of the value at a time, by columns
+      union {
+        uint2v h[2];
+        vec8 v;
+      } u;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = quad * 8 + e * 4 + (row >> 2), c = wave * 8 + t * 2 + (row >> 1 & 1);
+        u.h[e] = read_transposed(tile + (r * NC + (c ^ swizzle<NC>(r))) * 16 + (row & 1) * 8);
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) acc[b][t] = Elem<T>::mfma16(u.v, p[b], acc[b][t]);
+    }
+    there = there1;
+    there1 = there2;
+    buf = next;
+  }
+
+  // sums of the two halves of the keys
+  if (row_block < RB) {
+    l = sum_quarters(l);
+    if (quad == 0) s_sum[key_half][row_block * 16 + row] = l;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int32_t h = first_row + b * 16 + row, head = kv_head * a.group + h;
+    if (h >= a.group) continue;
+    const float sum = s_sum[0][b * 16 + row] + s_sum[1][b * 16 + row];
+    const int64_t slot = (2 * (int64_t)share + opens) * a.num_heads + head;
+    const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int d = wave * 64 + t * 16 + quad * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (d + e >= a.value_dim) continue;
+        if (whole)
+          static_cast<elem*>(a.out)[(int64_t)request * a.out_stride + (int64_t)head * a.value_dim + d + e] =
+              (elem)(sum == 0.f ? 0.f : acc[b][t][e] * inv);
+        else
+          plan.part[slot * a.value_dim + d + e] = acc[b][t][e];
+      }
+    }
+    if (wave == 0 && quad == 0) {
+      if (!whole) plan.part_ml[slot] = float2v{m[b], sum};
+      else if (a.lse)
+        a.lse[(int64_t)request * a.num_heads + head] = sum == 0.f ? -INFINITY : (m[b] + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+  __syncthreads();                                               // tiles and sums are free again
+  }
+}
+
+// Row blocks of 16 that a workgroup takes.
+int row_blocks(const Args& a) { return a.group <= 16 ? 1 : a.group <= 32 ? 2 : 4; }
+
+int32_t units(const Args& a) {
+  const int32_t rows = 16 * row_blocks(a);
+  return a.kv_heads * ((a.group + rows - 1) / rows);
+}
+
+int32_t wanted_shares(const Args& a) { return shares_for(a, kResident, units(a)); }
+
+template <int T, bool kF8>
+void launch(const Args& a, const Plan& p, hipStream_t stream) {
+  const int64_t items = p.shares > 0 ? p.shares : a.num_reqs;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8 * units(a))), block(kThreads);
+#define TOPKV_LATENT(RB)                                                                                                  \
+  do {                                                                                                                    \
+    if (p.shares > 0)                                                                                                     \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_latent_kernel<T, kF8, RB, true>), grid, block, 0, stream, a, p);    \
+    else                                                                                                                  \
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_latent_kernel<T, kF8, RB, false>), grid, block, 0, stream, a, p);   \
+  } while (0)
+  if (row_blocks(a) == 1) TOPKV_LATENT(1);
+  else if (row_blocks(a) == 2) TOPKV_LATENT(2);
+  else TOPKV_LATENT(4);
+#undef TOPKV_LATENT
+  launch_join(a, p, stream);
+}
+
+}  // namespace
+
+bool latent_takes(const Args& a) {
+  if (!rows_aligned(a) || a.value_bytes != 0 || a.head_dim <= 128 || a.head_dim > KD || a.value_dim > VD) return false;
+  const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
+  return items * units(a) <= INT32_MAX && (int64_t)wanted_shares(a) * a.num_heads <= INT32_MAX;
+}
+
+int64_t latent_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }
+
+topkv_status_t run_latent(const Args& a, void* workspace, hipStream_t stream) {
+  const Plan p = make_plan(a, wanted_shares(a), workspace);
+  if (a.kv_dtype == TOPKV_FP8_E4M3) {
+    if (a.dtype == TOPKV_BF16) launch<TOPKV_BF16, true>(a, p, stream);
+    else launch<TOPKV_FP16, true>(a, p, stream);
+  } else if (a.dtype == TOPKV_BF16) {
+    launch<TOPKV_BF16, false>(a, p, stream);
+  } else {
+    launch<TOPKV_FP16, false>(a, p, stream);
+  }
+  return hipGetLastError() == hipSuccess ? TOPKV_OK : TOPKV_ERR_LAUNCH;
+}
+
+}  // namespace topkv_attend

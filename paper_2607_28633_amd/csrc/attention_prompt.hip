@@ -97,8 +97,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   __shared__ int64_t s_base;
   __shared__ Rows s_rows;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = lane & 31, half = lane >> 5;
+  const int wave = threadIdx.x >> 6;
 
   // Eight row tiles (or shares) side by side over the eight XCDs, their KV heads one after the other on one XCD (whose
   // L2 then sees whole rows of the cache, and neighbouring row tiles the same keys).
@@ -146,6 +145,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   }
 
   while (at < upto) {
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   int32_t row_tile = (int32_t)(at - base);
   int32_t key_from = 0, key_to = INT32_MAX;                      // key tiles of this piece
   bool whole = true, opens = true;
