@@ -46,14 +46,17 @@ def attend_row(pool, table, position, q, kv_head, scale, value_dim, window=0, si
     return p @ values, top + np.log(total), p @ np.abs(values), float((scale * (np.abs(keys) @ np.abs(q))).max())
 
 
-def attend(pool, tables, seq_lens, q_starts, q, kv_heads, scale, value_dim, window=0, sinks=0, head_begin=0):
-    """Every row of q [tokens][heads][dim] that belongs to a request: dicts
-    keyed by (token, head) of attend_row's answers."""
+def attend(pool, tables, seq_lens, q_starts, q, kv_heads, scale, value_dim, window=0, sinks=0, head_begin=0, only=None):
+    """Every row of q [tokens][heads][dim] that belongs to a request (of the
+    tokens in `only`, if given): a dict keyed by (token, head) of attend_row's
+    answers."""
     heads = q.shape[1]
     got = {}
     for r, n in enumerate(seq_lens):
         first, last = int(q_starts[r]), int(q_starts[r + 1])
         for t in range(first, last):
+            if only is not None and t not in only:
+                continue
             position = int(n) - (last - t)
             for h in range(heads):
                 got[t, h] = attend_row(pool, tables[r], position, q[t, h], head_begin + h // (heads // kv_heads), scale,

@@ -1,9 +1,9 @@
 // attention_prompt.hip - many new tokens per request on the matrix units.
 //
-// A workgroup takes 128 query rows of one KV head, a row being one (token,
-// query head of the group): neighbouring tokens and all heads of the group
-// read the same keys, so even a short chunk fills the rows.  Four waves of 32
-// rows walk tiles of 64 keys: scores^T = K Q^T, running maximum and sum,
+// A workgroup takes 128 or 256 query rows of one KV head, a row being one
+// (token, query head of the group): neighbouring tokens and all heads of the
+// group read the same keys, so even a short chunk fills the rows.  Four or
+// eight waves of 32 rows walk tiles of 64 keys: scores^T = K Q^T, running maximum and sum,
 // out^T += V^T P^T, 4 * 32 * 64 * head_dim flops a wave and tile against
 // 256 * head_dim bytes of LDS: a wave's keys and values come out of LDS at the
 // rate at which the matrix units take them, and the softmax between the two
@@ -25,23 +25,22 @@ namespace topkv_attend {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 64;                // keys
 constexpr int kWaveRows = 32;
-constexpr int kRows = kWaves * kWaveRows;
+constexpr int kFew = 4, kMany = 8;       // waves of a workgroup
 // The maximum that scores are taken relative to follows only when it is this far behind (in powers of two): weights
 // stay below 2^8, which either 16-bit type holds as exactly as those below 1, and most tiles need no rescaling.
 constexpr float kSlack = 8.f;
 
 
-constexpr int resident(int KD) { return KD <= 64 ? 768 : KD <= 128 ? 512 : 256; }   // workgroups that 256 CUs hold at once
+constexpr int resident(int KD) { return KD <= 64 ? 768 : KD <= 128 ? 512 : 256; }   // workgroups of 4 waves that 256 CUs hold
 constexpr int kLeast = 4;                // key tiles of a share, at least
+constexpr int kCutRows = kFew * kWaveRows;
 
 struct Plan {
   int32_t most;        // row tiles that ascending q_starts can make
   int32_t shares;      // wanted; 0: a workgroup per row tile
-  float* part;         // [2 * share + 1 for a row tile's first piece][kv head][kRows][head_dim]
+  float* part;         // [2 * share + 1 for a row tile's first piece][kv head][kCutRows][head_dim]
   float2v* part_ml;    // the same without head_dim: maximum and sum
   int4* cut;           // [share]: request and first row of the row tile that starts in it and goes on, pieces (0: none)
 };
@@ -49,15 +48,17 @@ struct Plan {
 struct Rows {          // one request's new tokens
   int32_t first, count, shift;           // in q; shift: position of the first of them
 
-  __device__ int32_t tiles(const Args& a) const { return (int32_t)(((int64_t)count * a.group + kRows - 1) / kRows); }
+  template <int kRows> __device__ int32_t tiles(const Args& a) const {
+    return (int32_t)(((int64_t)count * a.group + kRows - 1) / kRows);
+  }
   // what the rows of row tile i see
-  __device__ Span span(const Args& a, int32_t i) const {
+  template <int kRows> __device__ Span span(const Args& a, int32_t i) const {
     const int64_t rows = (int64_t)count * a.group, last = (int64_t)(i + 1) * kRows < rows ? (int64_t)(i + 1) * kRows : rows;
     return key_span(a, shift + token_of(a, i * kRows), shift + token_of(a, (int32_t)last - 1));
   }
   // key tiles of the last row tile, at least 1: every row tile of the request counts as this many when work is shared out
-  __device__ int32_t depth(const Args& a) const {
-    const int32_t n = (span(a, tiles(a) - 1).count + kTile - 1) / kTile;
+  template <int kRows> __device__ int32_t depth(const Args& a) const {
+    const int32_t n = (span<kRows>(a, tiles<kRows>(a) - 1).count + kTile - 1) / kTile;
     return n < 1 ? 1 : n;
   }
 };
@@ -84,29 +85,32 @@ __device__ __forceinline__ uint4v without_special(uint4v w, bool* any) {
   return w;
 }
 
-template <int T, bool kF8, int KD, bool kCut>
-__global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_prompt_kernel(Args a, Plan plan) {
+constexpr int kAhead = 2;                // steps of the first product that keys are read ahead
+
+template <int T, bool kF8, int KD, int kWaves, bool kCut>
+__global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_prompt_kernel(Args a, Plan plan) {
   typedef typename Elem<T>::vec8 vec8;
   typedef typename Elem<T>::type elem;
+  constexpr int kThreads = 64 * kWaves, kRows = kWaveRows * kWaves;
   constexpr int NC = KD / 8;                                     // 16-byte chunks of a row in LDS
   constexpr int kLoads = kTile * NC / kThreads;                  // of a thread, for the keys and again for the values
   constexpr int kHalf = kTile * KD * 2;                          // bytes of a tile's keys
-  __shared__ __attribute__((aligned(16))) char s_tile[2][2 * kHalf];
-  __shared__ int32_t s_special[2][kWaves];
+  constexpr int kBuffers = kWaves == kMany && !kF8 ? 3 : 2;      // tiles in LDS: one in use, the others on their way
+  __shared__ __attribute__((aligned(16))) char s_tile[kBuffers][2 * kHalf];
+  __shared__ int32_t s_special[kBuffers][kWaves];
   __shared__ int32_t s_request;
   __shared__ int64_t s_base;
   __shared__ Rows s_rows;
 
   const int wave = threadIdx.x >> 6;
 
-  // Eight row tiles (or shares) side by side over the eight XCDs, their KV heads one after the other on one XCD (whose
-  // L2 then sees whole rows of the cache, and neighbouring row tiles the same keys).
-  const int32_t eight = blockIdx.x / (8 * a.kv_heads), within = blockIdx.x - eight * 8 * a.kv_heads;
-  const int32_t number = eight * 8 + (within & 7), kv_head = within >> 3;
+  // KV heads side by side: with 8 of them an XCD sees the keys and values of one, which its L2 then serves to all row
+  // tiles (8192 tokens, 8 heads of 128: 1251 us, against 1295 with all heads on every XCD).
+  const int32_t number = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - number * a.kv_heads;
   const auto weight = [&](int32_t r) -> int64_t {
     const Rows w = rows_of(a, r);
-    const int32_t n = w.tiles(a);
-    return kCut && n > 0 ? (int64_t)n * w.depth(a) : n;
+    const int32_t n = w.tiles<kRows>(a);
+    return kCut && n > 0 ? (int64_t)n * w.depth<kRows>(a) : n;
   };
   if (kCut && number >= plan.shares) return;
   if (threadIdx.x == 0) s_request = -1;
@@ -139,7 +143,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   constexpr int kChunkBytes = kF8 ? 8 : 16;
   typedef typename std::conditional<kF8, uint2v, uint4v>::type Raw;
   if (chunks < NC) {                                             // padding stays zero: loads leave it alone
-    for (int i = threadIdx.x; i < 2 * 2 * kHalf / 16; i += kThreads)
+    for (int i = threadIdx.x; i < kBuffers * 2 * kHalf / 16; i += kThreads)
       *reinterpret_cast<uint4v*>(&s_tile[0][0] + i * 16) = uint4v{0, 0, 0, 0};
     __syncthreads();
   }
@@ -150,11 +154,11 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   int32_t key_from = 0, key_to = INT32_MAX;                      // key tiles of this piece
   bool whole = true, opens = true;
   if constexpr (kCut) {
-    const int32_t depth = mine.depth(a);
+    const int32_t depth = mine.depth<kRows>(a);
     row_tile = (int32_t)((at - base) / depth);
     const int32_t from = (int32_t)((at - base) - (int64_t)row_tile * depth);
     const int32_t to = upto - at < depth - from ? from + (int32_t)(upto - at) : depth;
-    const int32_t have = (mine.span(a, row_tile).count + kTile - 1) / kTile;
+    const int32_t have = (mine.span<kRows>(a, row_tile).count + kTile - 1) / kTile;
     key_from = (int32_t)((int64_t)have * from / depth);
     key_to = (int32_t)((int64_t)have * to / depth);
     opens = from == 0;
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   const int32_t q_first = mine.first, shift = mine.shift;
   const int64_t rows = (int64_t)mine.count * a.group;
   const int32_t last_row = (int32_t)(first_row + kRows < rows ? first_row + kRows : rows) - 1;
-  const Span span = mine.span(a, row_tile);
+  const Span span = mine.span<kRows>(a, row_tile);
 
   // this lane's row, and the positions of the wave's rows
   const int32_t row = first_row + wave * kWaveRows + col;
@@ -243,9 +247,12 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   // The tile is in LDS for this wave's rows: rows without a key as zeros, whatever their place holds, and (watch) its
   // values' infinities and NaN as zeros too: times a weight of 0 they would reach rows that do not see their token.
   // Rows that do see it get them afterwards.
-  const auto settle = [&](int buf, uint64_t there, bool watch) {
+  const auto settle = [&](int buf, uint64_t there, bool watch, bool more) {
     if constexpr (!kF8) {
-      wait_loads();
+      // more: the loads of the tile after it are under way too (all of them: narrower rows may have a load without a
+      // lane to it, which is never issued)
+      if (kBuffers == 3 && more && chunks == NC) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * kLoads) : "memory");
+      else wait_loads();
       if (there == ~0ull && !watch) return;
     }
     bool special = false;
@@ -259,10 +266,11 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
         const uint4v none = {0, 0, 0, 0};
         if constexpr (kF8) {
           *k = is ? widen<T>(rk[i]) : none;
-          *v = is ? without_special<T>(widen<T>(rv[i]), &special) : none;
+          const uint4v w = widen<T>(rv[i]);
+          *v = !is ? none : watch ? without_special<T>(w, &special) : w;
         } else {
-          if (!is) *k = none;
-          *v = is ? without_special<T>(*v, &special) : none;
+          if (!is) *k = *v = none;
+          else if (watch) *v = without_special<T>(*v, &special);
         }
       }
     }
@@ -282,30 +290,37 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   const int32_t wg_first = shift + token_of(a, first_row), wg_last = shift + token_of(a, last_row);
   int64_t off = locate(begin, ask(begin));
   int32_t entry = ask(begin + kTile);
-  uint64_t there = __ballot(off >= 0), there_next = 0;
-  if (begin < count) {
-    fetch(0, off);
-    settle(0, there, !open(begin, wg_first, wg_last));
+  uint64_t there = __ballot(off >= 0), there1 = 0, there2 = 0;   // which keys the tile, the next and the one after it have
+  if (begin < count) fetch(0, off);
+  if constexpr (kBuffers == 3) {
+    off = locate(begin + kTile, entry);
+    entry = ask(begin + 2 * kTile);
+    there1 = __ballot(off >= 0);
+    if (begin + kTile < count) fetch(1, off);
   }
+  if (begin < count) settle(0, there, !open(begin, wg_first, wg_last), begin + kTile < count);
   if constexpr (kF8) {
     if (begin + kTile < count) {
       off = locate(begin + kTile, entry);
       entry = ask(begin + 2 * kTile);
-      there_next = __ballot(off >= 0);
+      there1 = __ballot(off >= 0);
       fetch(1, off);
     }
   }
   __syncthreads();
 
-  for (int32_t first = begin, buf = 0; first < count; first += kTile, buf ^= 1) {
+  int buf = 0;
+  for (int32_t first = begin; first < count; first += kTile) {
+    const int next = buf + 1 < kBuffers ? buf + 1 : 0;
     const char* keys = s_tile[buf];
     const char* values = keys + kHalf;
     if constexpr (!kF8) {
-      if (first + kTile < count) {
-        off = locate(first + kTile, entry);
-        entry = ask(first + 2 * kTile);
-        there_next = __ballot(off >= 0);
-        fetch(buf ^ 1, off);
+      constexpr int kOn = (kBuffers - 1) * kTile;
+      if (first + kOn < count) {
+        off = locate(first + kOn, entry);
+        entry = ask(first + kOn + kTile);
+        (kBuffers == 3 ? there2 : there1) = __ballot(off >= 0);
+        fetch(kBuffers == 2 ? next : next + 1 < kBuffers ? next + 1 : 0, off);
       }
     }
     // tiles behind the wave's last row, or (their last key) before its first row's window, are nothing to it
@@ -313,17 +328,32 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
     const int32_t k_last = key_position(span, first + kTile - 1 < count ? first + kTile - 1 : count - 1);
     const bool use = k_first <= wave_last && (a.window == 0 || k_last > wave_first - a.window || k_first < a.sinks);
     if (use) {
+      // Keys leave LDS a few steps ahead of their product, values and weights one step ahead of theirs: the scheduling
+      // barriers hold that order, which the compiler gives up for fewer registers (a product then waits for LDS each time).
       float16v x[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[b][i] = 0.f;
+      const auto key = [&](int b, int s) {
         const int r = b * 32 + col;
+        return *reinterpret_cast<const vec8*>(keys + (r * NC + ((s * 2 + half) ^ swizzle<NC>(r))) * 16);
+      };
+      constexpr int kSteps = KD / 16;
+      vec8 k[kAhead + 1][2];
 #pragma unroll
-        for (int s = 0; s < KD / 16; ++s) {
-          const vec8 k = *reinterpret_cast<const vec8*>(keys + (r * NC + ((s * 2 + half) ^ swizzle<NC>(r))) * 16);
-          x[b] = Elem<T>::mfma32(k, q[s], x[b]);
-        }
+      for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) k[s][b] = key(b, s);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if (s + kAhead < kSteps)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) k[(s + kAhead) % (kAhead + 1)][b] = key(b, s + kAhead);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) x[b] = Elem<T>::mfma32(k[s % (kAhead + 1)][b], q[s], x[b]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const bool clear = there == ~0ull && open(first, wave_first, wave_last);
       if (!clear) {
@@ -354,15 +384,17 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
         for (int t = 0; t < KD / 32; ++t) acc[t] *= fall;
       }
       const float base = m == -INFINITY ? 0.f : m;
-      vec8 p[4];                                                 // 16 keys each
+      // weights of 16 keys
+      const auto weigh = [&](int s) {
+        vec8 p;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], a.scale, -base));
+        for (int i = 0; i < 8; ++i) {
+          const float w = __builtin_amdgcn_exp2f(fmaf(x[s >> 1][(s & 1) * 8 + i], a.scale, -base));
           l += w;
-          p[b * 2 + (i >> 3)][i & 7] = (elem)w;                  // rounded for the matrix units, its sum is not
+          p[i] = (elem)w;                                        // rounded for the matrix units, its sum is not
         }
+        return p;
+      };
       // values by columns: lane (d, half) takes keys 4 half .. + 3 of each eight, as the weights lie
       const auto column = [&](int t, int s) {
         union {
@@ -376,10 +408,24 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
         }
         return u.v;
       };
+      constexpr int kWide = KD / 32 < 4 ? KD / 32 : 4;           // 32-element columns of a step
+      constexpr int kTurns = KD / 32 / kWide;                    // steps of the same 16 keys
+      vec8 v[2][kWide], p[2];
 #pragma unroll
-      for (int t = 0; t < KD / 32; ++t)
+      for (int t = 0; t < kWide; ++t) v[0][t] = column(t, 0);
+      p[0] = weigh(0);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) acc[t] = Elem<T>::mfma32(column(t, s), p[s], acc[t]);
+      for (int n = 0; n < 4 * kTurns; ++n) {
+        const int s = n / kTurns, u = n % kTurns;
+        if (n + 1 < 4 * kTurns)
+#pragma unroll
+          for (int t = 0; t < kWide; ++t) v[(n + 1) & 1][t] = column((n + 1) % kTurns * kWide + t, (n + 1) / kTurns);
+#pragma unroll
+        for (int t = 0; t < kWide; ++t) acc[u * kWide + t] = Elem<T>::mfma32(v[n & 1][t], p[s & 1], acc[u * kWide + t]);
+        if (u == 0 && s + 1 < 4) p[(s + 1) & 1] = weigh(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       if (!clear) {
         int special = 0;
 #pragma unroll
@@ -406,16 +452,19 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
         }
       }
     }
-    there = there_next;
-    if (first + kTile < count) settle(buf ^ 1, there, !open(first + kTile, wg_first, wg_last));
+    if (first + kTile < count)
+      settle(next, there1, !open(first + kTile, wg_first, wg_last), first + 2 * kTile < count);
+    there = there1;
+    if constexpr (kBuffers == 3) there1 = there2;
     if constexpr (kF8) {
       if (first + 2 * kTile < count) {
         off = locate(first + 2 * kTile, entry);
         entry = ask(first + 3 * kTile);
-        there_next = __ballot(off >= 0);
+        there1 = __ballot(off >= 0);
         fetch(buf, off);
       }
     }
+    buf = next;
     __syncthreads();
   }
 
@@ -465,7 +514,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
   }
   if constexpr (kCut) {
     // on to the next row tile, of a later request where this one's are done
-    if (at < upto && at == base + (int64_t)mine.tiles(a) * mine.depth(a)) {
+    if (at < upto && at == base + (int64_t)mine.tiles<kRows>(a) * mine.depth<kRows>(a)) {
       base = at;
       do mine = rows_of(a, ++request);
       while (mine.count == 0 && request + 1 < a.num_reqs);
@@ -477,19 +526,19 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_pro
 // Row tiles in pieces: a workgroup for 16 rows of (share that one starts in,
 // KV head), a wave for 4 of them.
 template <int T>
-__global__ __launch_bounds__(kThreads) void kv_attention_prompt_join_kernel(Args a, Plan plan) {
+__global__ __launch_bounds__(256) void kv_attention_prompt_join_kernel(Args a, Plan plan) {
   const int32_t share = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - share * a.kv_heads;
   const int4 cut = plan.cut[share];
   if (cut.z == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Rows mine = rows_of(a, cut.x);
-  const int64_t step = (int64_t)a.kv_heads * kRows;
+  const int64_t step = (int64_t)a.kv_heads * kCutRows;
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {
     const int32_t in_tile = blockIdx.y * 16 + wave * 4 + i, row = cut.y + in_tile;
     if (row >= (int64_t)mine.count * a.group) return;
     const int32_t token = token_of(a, row), head = kv_head * a.group + (row - token * a.group);
-    const int64_t slot = (2 * (int64_t)share * a.kv_heads + kv_head) * kRows + in_tile;   // piece k: 2 k steps on, the first 1
+    const int64_t slot = (2 * (int64_t)share * a.kv_heads + kv_head) * kCutRows + in_tile;   // piece k: 2 k steps on, the first 1
     float top = -INFINITY;
     for (int32_t k = lane; k < cut.z; k += 64) top = fmaxf(top, plan.part_ml[slot + (k ? 2 * k : 1) * step][0]);
 #pragma unroll
@@ -519,39 +568,60 @@ __global__ __launch_bounds__(kThreads) void kv_attention_prompt_join_kernel(Args
 }
 
 // Row tiles that any division of the rows among the requests can make, and that every one makes.
-int64_t most_tiles(const Args& a) { return (int64_t)a.total_q * a.group / kRows + a.num_reqs; }
-int64_t least_tiles(const Args& a) { return ((int64_t)a.total_q * a.group + kRows - 1) / kRows; }
+int64_t most_tiles(const Args& a, int waves) { return (int64_t)a.total_q * a.group / (waves * kWaveRows) + a.num_reqs; }
+int64_t least_tiles(const Args& a, int waves) {
+  return ((int64_t)a.total_q * a.group + waves * kWaveRows - 1) / (waves * kWaveRows);
+}
+
+int64_t most_keys(const Args& a) {
+  const int64_t seen = (int64_t)a.bt_stride * a.page_size;
+  return a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
+}
+
+// Eight waves on one tile halve the loads of a row and have two tiles on their way, four waves twice over a CU start
+// and end more easily.  8192 tokens, heads of 128: 8 waves 1203 us, 4 1292; windows of 128, heads of 64: 250 and 180.
+// Heads of 256 have no registers for more than one wave a SIMD.
+int waves_for(const Args& a) {
+  return a.head_dim > 64 && a.head_dim <= 128 && most_keys(a) >= 1024 &&
+                 least_tiles(a, kMany) * a.kv_heads >= resident(a.head_dim)
+             ? kMany
+             : kFew;
+}
 
 // Shares of the work, 0 where the row tiles are enough: twice as many as fit the GPU at once, so that the last of them
 // leave little of it idle; or where no row can see more keys than a share should have.
 int32_t wanted_shares(const Args& a) {
-  const int64_t fit = resident(a.head_dim), seen = (int64_t)a.bt_stride * a.page_size;
-  const int64_t most = a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
-  if (least_tiles(a) * a.kv_heads >= 2 * fit || most <= 2 * kLeast * kTile) return 0;
+  const int64_t fit = resident(a.head_dim);
+  if (least_tiles(a, kFew) * a.kv_heads >= 2 * fit || most_keys(a) <= 2 * kLeast * kTile) return 0;
   const int32_t n = (int32_t)(fit / a.kv_heads);
   return n < 1 ? 1 : n;
 }
 
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
 
+template <int T, bool kF8, int KD, int kWaves, bool kCut>
+void launch_one(const Args& a, const Plan& p, int64_t items, hipStream_t stream) {
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, KD, kWaves, kCut>), dim3((unsigned)(items * a.kv_heads)),
+                     dim3(64 * kWaves), 0, stream, a, p);
+}
+
 template <int T, bool kF8>
 void launch(const Args& a, const Plan& p, hipStream_t stream) {
-  const int64_t items = p.shares > 0 ? p.shares : p.most;
-  const dim3 grid((unsigned)((items + 7) / 8 * 8 * a.kv_heads)), block(kThreads);
-#define TOPKV_PROMPT(KD)                                                                                                 \
-  do {                                                                                                                   \
-    if (p.shares > 0)                                                                                                    \
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, KD, true>), grid, block, 0, stream, a, p);   \
-    else                                                                                                                 \
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_kernel<T, kF8, KD, false>), grid, block, 0, stream, a, p);  \
-  } while (0)
-  if (a.head_dim <= 64) TOPKV_PROMPT(64);
-  else if (a.head_dim <= 128) TOPKV_PROMPT(128);
-  else TOPKV_PROMPT(256);
-#undef TOPKV_PROMPT
-  if (p.shares > 0)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_join_kernel<T>), dim3((unsigned)(p.shares * a.kv_heads), kRows / 16),
-                       block, 0, stream, a, p);
+  if (p.shares > 0) {
+    if (a.head_dim <= 64) launch_one<T, kF8, 64, kFew, true>(a, p, p.shares, stream);
+    else if (a.head_dim <= 128) launch_one<T, kF8, 128, kFew, true>(a, p, p.shares, stream);
+    else launch_one<T, kF8, 256, kFew, true>(a, p, p.shares, stream);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_join_kernel<T>), dim3((unsigned)(p.shares * a.kv_heads), kCutRows / 16),
+                       dim3(256), 0, stream, a, p);
+  } else if (a.head_dim <= 64) {
+    launch_one<T, kF8, 64, kFew, false>(a, p, p.most, stream);
+  } else if (waves_for(a) == kMany) {
+    launch_one<T, kF8, 128, kMany, false>(a, p, p.most, stream);
+  } else if (a.head_dim <= 128) {
+    launch_one<T, kF8, 128, kFew, false>(a, p, p.most, stream);
+  } else {
+    launch_one<T, kF8, 256, kFew, false>(a, p, p.most, stream);
+  }
 }
 
 }  // namespace
@@ -560,21 +630,21 @@ bool prompt_takes(const Args& a) {
   const int64_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
   if (a.value_bytes == 0 || a.head_dim % 8 != 0 || a.head_dim > 256) return false;
   if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
-  const int64_t items = most_tiles(a) > wanted_shares(a) ? most_tiles(a) : wanted_shares(a);
-  return (items + 8) * a.kv_heads <= INT32_MAX;
+  const int64_t items = most_tiles(a, kFew) > wanted_shares(a) ? most_tiles(a, kFew) : wanted_shares(a);
+  return items * a.kv_heads <= INT32_MAX;
 }
 
 int64_t prompt_workspace(const Args& a) {
-  const int64_t shares = ((int64_t)wanted_shares(a) + 7) / 8 * 8, rows = 2 * shares * a.kv_heads * kRows;
+  const int64_t shares = wanted_shares(a), rows = 2 * shares * a.kv_heads * kCutRows;
   return up16(rows * a.head_dim * 4) + up16(rows * 8) + shares * 16;
 }
 
 topkv_status_t run_prompt(const Args& a, void* workspace, hipStream_t stream) {
   Plan p = {};
-  p.most = (int32_t)most_tiles(a);
   p.shares = wanted_shares(a);
+  p.most = (int32_t)most_tiles(a, p.shares > 0 ? kFew : waves_for(a));
   if (p.shares > 0) {
-    const int64_t shares = ((int64_t)p.shares + 7) / 8 * 8, rows = 2 * shares * a.kv_heads * kRows;
+    const int64_t rows = 2 * (int64_t)p.shares * a.kv_heads * kCutRows;
     char* at = static_cast<char*>(workspace);
     p.part = reinterpret_cast<float*>(at);
     at += up16(rows * a.head_dim * 4);

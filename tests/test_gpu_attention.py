@@ -65,12 +65,12 @@ class Case:
         self.scale = 1.0 / np.sqrt(dim)
         self.k_scale, self.v_scale = (0.75, 1.25) if kv_type == F8 else (1.0, 1.0)
 
-    def exact(self, rows=None):
+    def exact(self, only=None):
         pool = self.pool.to(torch.float64).numpy()
         pool = pool * self.k_scale
         got = attend(pool, self.tables, [max(0, min(n, self.tables.shape[1] * self.page)) for n in self.lens], self.starts,
                      self.q.to(torch.float64).numpy(), self.kv, self.scale, self.value, self.window, self.sinks,
-                     self.head_begin)
+                     self.head_begin, only)
         return {k: (o * (self.v_scale / self.k_scale), l, s * abs(self.v_scale / self.k_scale), b)
                 for k, (o, l, s, b) in got.items()}
 
@@ -185,6 +185,36 @@ def test_prompt(tk, shape, mask):
              **MASKS[mask]).device(tk)
     c.call(tk)
     c.check()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(dim=96, q_type=FP, kv_type=FP), dict(kv_type=F8), dict(window=1500, sinks=5),
+                                dict(dim=120, page=24, major="head"), dict(dim=64), dict(dim=256, kv=4), dict(group=3, kv=16)])
+def test_prompt_large(tk, kw):
+    """Prompts that fill the GPU by themselves, with absent pages and tokens of NaN; rows checked at random and around
+    those and the prompts' ends."""
+    say(f"[attention] large prompt {kw}")
+    lens = [2230, 1, 700, 65]
+    c = Case(37, lens, lens, **{**dict(kv=8, group=8), **kw})
+    rng = np.random.default_rng(1)
+    c.tables[0, 300 // c.page] = -1
+    c.tables[2, 650 // c.page] = 2**31 - 1
+    page = c.pool[int(c.tables[0, 1500 // c.page])].to(torch.float32)
+    page[-1, 1500 % c.page] = float("nan")                            # the value of token 1500
+    c.pool[int(c.tables[0, 1500 // c.page])] = page.to(c.kv_type)
+    c.device(tk)
+    c.call(tk)
+    first = int(c.starts[2])
+    only = {0, 1, 62, 63, 64, 299, 320, 1400, 1490, 1498, 1499, 2230, 2231, first + 699, first + 650, first + 700}
+    only |= set(rng.integers(0, 1500, 8).tolist()) | set((first + rng.integers(0, 700, 8)).tolist())
+    with np.errstate(invalid="ignore"):
+        c.check(c.exact(only=only))
+    assert not torch.isfinite(c.out_d[1500].float()).any() and not torch.isfinite(c.out_d[1700].float()).any()
+    c.out_full.fill_(77), c.lse_d.fill_(77)
+    before = c.out_full.clone()
+    c.call(tk)
+    first_run = c.out_full.clone()
+    c.call(tk)
+    assert torch.equal(torch.nan_to_num(first_run), torch.nan_to_num(c.out_full)) and not torch.equal(before, c.out_full)
 
 
 @pytest.mark.parametrize("lens,kw", [([5000], {}), ([20011, 3, 900], dict(group=8, kv=1)), ([4097] * 3, dict(kv_type=F8)),
