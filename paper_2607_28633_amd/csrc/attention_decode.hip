@@ -279,10 +279,8 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
     }
     const int32_t head = kv_head * a.group + first_row + r;
     if (!whole) {
-      const int64_t slot = ((2 * (int64_t)share + opens) * a.kv_heads + kv_head) * a.group + first_row + r;
-      float* out = plan.part + slot * a.value_dim + d;
-      for (int e = 0; e < 4; ++e)
-        if (d + e < a.value_dim) out[e] = o[e];
+      const int64_t slot = (2 * (int64_t)share + opens) * a.num_heads + head;
+      *reinterpret_cast<float4v*>(plan.part + slot * plan.part_dim + d) = o;
       if (d == 0) plan.part_ml[slot] = float2v{top, sum};
     } else {
       const float inv = sum == 0.f ? 0.f : a.v_scale / sum;

@@ -290,15 +290,14 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int d = wave * 64 + t * 16 + quad * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (d + e >= a.value_dim) continue;
-        if (whole)
-          static_cast<elem*>(a.out)[(int64_t)request * a.out_stride + (int64_t)head * a.value_dim + d + e] =
-              (elem)(sum == 0.f ? 0.f : acc[b][t][e] * inv);
-        else
-          plan.part[slot * a.value_dim + d + e] = acc[b][t][e];
+      if (!whole) {
+        if (d < plan.part_dim) *reinterpret_cast<float4v*>(plan.part + slot * plan.part_dim + d) = acc[b][t];
+        continue;
       }
+      elem* out = static_cast<elem*>(a.out) + (int64_t)request * a.out_stride + (int64_t)head * a.value_dim + d;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d + e < a.value_dim) out[e] = (elem)(sum == 0.f ? 0.f : acc[b][t][e] * inv);
     }
     if (wave == 0 && quad == 0) {
       if (!whole) plan.part_ml[slot] = float2v{m[b], sum};

@@ -524,47 +524,59 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
 }
 
 // Row tiles in pieces: a workgroup for 16 rows of (share that one starts in,
-// KV head), a wave for 4 of them.
+// KV head), 16 lanes a row with 8 elements each, so that every load of a wave
+// is whole lines and no row waits for another.
 template <int T>
 __global__ __launch_bounds__(256) void kv_attention_prompt_join_kernel(Args a, Plan plan) {
+  typedef typename Elem<T>::type elem;
   const int32_t share = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - share * a.kv_heads;
   const int4 cut = plan.cut[share];
   if (cut.z == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Rows mine = rows_of(a, cut.x);
+  const int32_t in_tile = blockIdx.y * 16 + (threadIdx.x >> 4), row = cut.y + in_tile;
+  if (row >= (int64_t)mine.count * a.group) return;
+  const int32_t token = token_of(a, row), head = kv_head * a.group + (row - token * a.group);
   const int64_t step = (int64_t)a.kv_heads * kCutRows;
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    const int32_t in_tile = blockIdx.y * 16 + wave * 4 + i, row = cut.y + in_tile;
-    if (row >= (int64_t)mine.count * a.group) return;
-    const int32_t token = token_of(a, row), head = kv_head * a.group + (row - token * a.group);
-    const int64_t slot = (2 * (int64_t)share * a.kv_heads + kv_head) * kCutRows + in_tile;   // piece k: 2 k steps on, the first 1
-    float top = -INFINITY;
-    for (int32_t k = lane; k < cut.z; k += 64) top = fmaxf(top, plan.part_ml[slot + (k ? 2 * k : 1) * step][0]);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  const int64_t slot = (2 * (int64_t)share * a.kv_heads + kv_head) * kCutRows + in_tile;   // piece k: 2 k steps on, the first 1
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int32_t k = 0; k < cut.z; ++k) top = fmaxf(top, plan.part_ml[slot + (k ? 2 * k : 1) * step][0]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  elem* out = static_cast<elem*>(a.out) + (int64_t)(mine.first + token) * a.out_stride + (int64_t)head * a.value_dim;
+  for (int32_t d = (threadIdx.x & 15) * 8; d < a.head_dim; d += 128) {
+    float4v lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+    sum = 0.f;
 #pragma unroll 4
     for (int32_t k = 0; k < cut.z; ++k) {
       const int64_t s = slot + (k ? 2 * k : 1) * step;
       const float2v ml = plan.part_ml[s];
       const float f = __builtin_amdgcn_exp2f(ml[0] - base);
+      const float4v* from = reinterpret_cast<const float4v*>(plan.part + s * a.head_dim + d);
       sum = fmaf(f, ml[1], sum);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e * 64 + lane < a.head_dim) o[e] = fmaf(f, plan.part[s * a.head_dim + e * 64 + lane], o[e]);
+      lo += from[0] * f;
+      hi += from[1] * f;
     }
     const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
-    typename Elem<T>::type* out = static_cast<typename Elem<T>::type*>(a.out) + (int64_t)(mine.first + token) * a.out_stride +
-                                  (int64_t)head * a.value_dim;
+    union {
+      elem e[8];
+      uint4v w;
+    } u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e * 64 + lane < a.head_dim) out[e * 64 + lane] = (typename Elem<T>::type)(sum == 0.f ? 0.f : o[e] * inv);
-    if (a.lse && lane == 0)
-      a.lse[(int64_t)(mine.first + token) * a.num_heads + head] =
-          sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int i = 0; i < 4; ++i) {
+      u.e[i] = (elem)(sum == 0.f ? 0.f : lo[i] * inv);
+      u.e[i + 4] = (elem)(sum == 0.f ? 0.f : hi[i] * inv);
+    }
+    if (a.out_wide) {
+      *reinterpret_cast<uint4v*>(out + d) = u.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[d + i] = u.e[i];
+    }
   }
+  if (a.lse && (threadIdx.x & 15) == 0)
+    a.lse[(int64_t)(mine.first + token) * a.num_heads + head] =
+        sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // Row tiles that any division of the rows among the requests can make, and that every one makes.
