@@ -149,7 +149,9 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   }
 
   while (at < upto) {
-  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  int lane = threadIdx.x & 63;
+  if constexpr (kCut) asm volatile("" : "+v"(lane));             // addresses made from it stay in the loop: registers
+  const int col = lane & 31, half = lane >> 5;
   int32_t row_tile = (int32_t)(at - base);
   int32_t key_from = 0, key_to = INT32_MAX;                      // key tiles of this piece
   bool whole = true, opens = true;
@@ -221,6 +223,12 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
     const uint32_t j = (uint32_t)key_position(span, v);
     return (int64_t)entry * a.page_bytes + (int64_t)(j - page_of(a, j) * (uint32_t)a.page_size) * a.slot_bytes;
   };
+  // The lane again, where addresses made from it had better be made anew in every tile than be kept.
+  const auto near = [&]() -> int {
+    int here = lane;
+    if constexpr (kCut || KD > 128) asm volatile("" : "+v"(here));
+    return here;
+  };
   const auto from_of = [&](int64_t off, int r) {
     const int lo = off < 0 ? 0 : (int)(uint32_t)off, hi = off < 0 ? 0 : (int)(off >> 32);
     return cache + (int64_t)((uint64_t)(uint32_t)__shfl(hi, r, 64) << 32 | (uint32_t)__shfl(lo, r, 64));
@@ -229,6 +237,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   // 16 bytes behind the other by lane, so the swizzle is in which chunk a lane asks for.
   Raw rk[kF8 ? kLoads : 1], rv[kF8 ? kLoads : 1];
   const auto fetch = [&](int buf, int64_t off) {
+    const int lane = near();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int place = (wave * kLoads + i) * 64 + lane, r = place / NC, c = (place - r * NC) ^ swizzle<NC>(r);
@@ -256,6 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
       if (there == ~0ull && !watch) return;
     }
     bool special = false;
+    const int lane = near();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int place = (wave * kLoads + i) * 64 + lane, r = place / NC, c = (place - r * NC) ^ swizzle<NC>(r);
@@ -335,6 +345,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[b][i] = 0.f;
+      const int lane = near(), col = lane & 31, half = lane >> 5;
       const auto key = [&](int b, int s) {
         const int r = b * 32 + col;
         return *reinterpret_cast<const vec8*>(keys + (r * NC + ((s * 2 + half) ^ swizzle<NC>(r))) * 16);
@@ -408,7 +419,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
         }
         return u.v;
       };
-      constexpr int kWide = KD / 32 < 4 ? KD / 32 : 4;           // 32-element columns of a step
+      constexpr int kWide = KD == 128 ? 4 : 2;                   // 32-element columns of a step
       constexpr int kTurns = KD / 32 / kWide;                    // steps of the same 16 keys
       vec8 v[2][kWide], p[2];
 #pragma unroll
