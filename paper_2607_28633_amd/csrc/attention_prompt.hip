@@ -87,6 +87,50 @@ __device__ __forceinline__ uint4v without_special(uint4v w, bool* any) {
 
 constexpr int kAhead = 2;                // steps of the first product that keys are read ahead
 
+// Whether cutting row tiles along the keys takes less time than leaving them whole, both estimated in key tiles of a
+// workgroup alone on its CU (1.8 us; two on a CU take 1.4 as long each).  Whole: the deepest row tile, or the work of
+// all over the workgroups that fit.  Cut: an equal share, and for shorter prologues, partial results and the join 8 and
+// up to 12 more, by how many pieces there are.  One request, 8 KV heads of 4, 3000 new tokens: whole 100 us, cut 217;
+// 64 new tokens of 3000: 92 and 37.
+template <int kWaves, int KD>
+__device__ bool pays(const Args& a) {
+  constexpr int kRows = kWaveRows * kWaves;
+  __shared__ float s_units[kWaves], s_work[kWaves], s_deep[kWaves], s_tiles[kWaves];
+  float units = 0.f, work = 0.f, deep = 0.f, tiles = 0.f;
+  for (int32_t r = threadIdx.x; r < a.num_reqs; r += 64 * kWaves) {
+    const Rows w = rows_of(a, r);
+    const int32_t n = w.tiles<kRows>(a);
+    if (n == 0) continue;
+    const float d = (float)w.depth<kRows>(a), first = (float)((w.span<kRows>(a, 0).count + kTile - 1) / kTile);
+    tiles += n;
+    units += n * d;
+    work += n * 0.5f * (first + d);
+    deep = fmaxf(deep, d);
+  }
+#pragma unroll
+  for (int i = 32; i; i >>= 1) {
+    units += __shfl_xor(units, i, 64);
+    work += __shfl_xor(work, i, 64);
+    tiles += __shfl_xor(tiles, i, 64);
+    deep = fmaxf(deep, __shfl_xor(deep, i, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    const int w = threadIdx.x >> 6;
+    s_units[w] = units, s_work[w] = work, s_deep[w] = deep, s_tiles[w] = tiles;
+  }
+  __syncthreads();
+  units = work = deep = tiles = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    units += s_units[w], work += s_work[w], tiles += s_tiles[w];
+    deep = fmaxf(deep, s_deep[w]);
+  }
+  const float fit = (float)resident(KD), heads = (float)a.kv_heads, slow = tiles * heads <= 256.f ? 1.f : 1.4f;
+  const float share = units * heads / fit, whole = fmaxf(deep, work * heads / fit) * slow;
+  const float cut = fmaxf(share, (float)kLeast) * 1.4f + 8.f + 12.f * fminf(1.f, share / kLeast);
+  return cut < whole;
+}
+
 template <int T, bool kF8, int KD, int kWaves, bool kCut>
 __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_prompt_kernel(Args a, Plan plan) {
   typedef typename Elem<T>::vec8 vec8;
@@ -107,21 +151,25 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   // KV heads side by side: with 8 of them an XCD sees the keys and values of one, which its L2 then serves to all row
   // tiles (8192 tokens, 8 heads of 128: 1251 us, against 1295 with all heads on every XCD).
   const int32_t number = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - number * a.kv_heads;
+  bool cutting = false;                                          // whether this batch is cut: the same for all workgroups
+  if constexpr (kCut) {
+    if (number < plan.shares && kv_head == 0 && threadIdx.x == 0) plan.cut[number] = make_int4(0, 0, 0, 0);
+    cutting = pays<kWaves, KD>(a);
+    if (cutting && number >= plan.shares) return;
+  }
   const auto weight = [&](int32_t r) -> int64_t {
     const Rows w = rows_of(a, r);
     const int32_t n = w.tiles<kRows>(a);
-    return kCut && n > 0 ? (int64_t)n * w.depth<kRows>(a) : n;
+    return cutting && n > 0 ? (int64_t)n * w.depth<kRows>(a) : n;
   };
-  if (kCut && number >= plan.shares) return;
   if (threadIdx.x == 0) s_request = -1;
   Scan<int64_t> scan = scan_requests<int64_t, kWaves>(a.num_reqs, weight);
   int64_t size = 1, at, upto;
-  if constexpr (kCut) {
+  if (cutting) {
     size = (scan.total + plan.shares - 1) / plan.shares;
     size = size < kLeast ? kLeast : size;
     at = number * size;
     upto = at + size < scan.total ? at + size : scan.total;
-    if (kv_head == 0 && threadIdx.x == 0) plan.cut[number] = make_int4(0, 0, 0, 0);
   } else {
     if (scan.total > plan.most) return;                          // q_starts do not ascend
     at = scan.total - 1 - number;                                // the last, longest first
@@ -155,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   int32_t row_tile = (int32_t)(at - base);
   int32_t key_from = 0, key_to = INT32_MAX;                      // key tiles of this piece
   bool whole = true, opens = true;
-  if constexpr (kCut) {
+  if (cutting) {
     const int32_t depth = mine.depth<kRows>(a);
     row_tile = (int32_t)((at - base) / depth);
     const int32_t from = (int32_t)((at - base) - (int64_t)row_tile * depth);
@@ -523,7 +571,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
     if (real && a.lse && half == 0)
       a.lse[(int64_t)(q_first + token) * a.num_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
-  if constexpr (kCut) {
+  if (cutting) {
     // on to the next row tile, of a later request where this one's are done
     if (at < upto && at == base + (int64_t)mine.tiles<kRows>(a) * mine.depth<kRows>(a)) {
       base = at;
@@ -611,8 +659,8 @@ int waves_for(const Args& a) {
              : kFew;
 }
 
-// Shares of the work, 0 where the row tiles are enough: twice as many as fit the GPU at once, so that the last of them
-// leave little of it idle; or where no row can see more keys than a share should have.
+// Shares of the work where it may be cut, which the kernel decides by the lengths; 0 where the row tiles are enough for
+// certain (twice as many as fit the GPU at once) or no row can see more keys than two shares should have.
 int32_t wanted_shares(const Args& a) {
   const int64_t fit = resident(a.head_dim);
   if (least_tiles(a, kFew) * a.kv_heads >= 2 * fit || most_keys(a) <= 2 * kLeast * kTile) return 0;
@@ -631,9 +679,10 @@ void launch_one(const Args& a, const Plan& p, int64_t items, hipStream_t stream)
 template <int T, bool kF8>
 void launch(const Args& a, const Plan& p, hipStream_t stream) {
   if (p.shares > 0) {
-    if (a.head_dim <= 64) launch_one<T, kF8, 64, kFew, true>(a, p, p.shares, stream);
-    else if (a.head_dim <= 128) launch_one<T, kF8, 128, kFew, true>(a, p, p.shares, stream);
-    else launch_one<T, kF8, 256, kFew, true>(a, p, p.shares, stream);
+    const int64_t items = p.most > p.shares ? p.most : p.shares;   // the kernel finds out which of them are wanted
+    if (a.head_dim <= 64) launch_one<T, kF8, 64, kFew, true>(a, p, items, stream);
+    else if (a.head_dim <= 128) launch_one<T, kF8, 128, kFew, true>(a, p, items, stream);
+    else launch_one<T, kF8, 256, kFew, true>(a, p, items, stream);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_prompt_join_kernel<T>), dim3((unsigned)(p.shares * a.kv_heads), kCutRows / 16),
                        dim3(256), 0, stream, a, p);
   } else if (a.head_dim <= 64) {
