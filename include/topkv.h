@@ -667,10 +667,11 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
  *   lse:       device float[num_reqs][num_heads], or NULL
  *   workspace: device memory, 16-byte aligned (may be NULL when
  *              topkv_attention_workspace_bytes is 0)
- * num_reqs == 0 launches nothing.  Any head_dim up to 1024; rows of q, out
- * and the cache that are multiples of 16 bytes (8 for an 8-bit cache) on such
- * addresses with head_dim up to 256 (planes 1: up to 576) run on the matrix
- * units, others on a slower general kernel.  Errors: TOPKV_ERR_INVALID_ARG for bad
+ * num_reqs == 0 launches nothing.  Any head_dim up to 1024: where it is a
+ * multiple of 8 up to 256 (planes 1: up to 576, with value_dim up to 512) and
+ * q's and the cache's rows lie on 16-byte addresses (the cache's on 8-byte
+ * ones when it is 8-bit) the matrix units do the work, elsewhere a slower
+ * general kernel.  Errors: TOPKV_ERR_INVALID_ARG for bad
  * descriptors, options, null pointers or a short or misaligned workspace,
  * TOPKV_ERR_UNSUPPORTED for head_dim above 1024, more than
  * TOPKV_MAX_BATCH_REQS requests, bt_stride * page_size of 2^30 or more,
@@ -688,8 +689,8 @@ topkv_status_t topkv_attention_decode(const topkv_view_t* cache, const topkv_att
  *   total_q:   rows of q, out and lse; rows that belong to no request are
  *              left as they were
  * A token whose position would be negative (more new tokens than seq_lens[r])
- * sees nothing.  Otherwise as topkv_attention_decode; total_q == 0 launches
- * nothing. */
+ * sees nothing.  Otherwise as topkv_attention_decode, but latent caches
+ * (planes 1) run on the general kernel; total_q == 0 launches nothing. */
 topkv_status_t topkv_attention_prompt(const topkv_view_t* cache, const topkv_attention_t* attn,
                                       int32_t num_reqs, const int32_t* seq_lens, const int32_t* q_starts,
                                       int32_t total_q, const void* q, void* out, float* lse, void* workspace,
@@ -708,7 +709,7 @@ typedef struct topkv_page_owner {
   int32_t* seq_lens;      /* device int32[num_rows] */
   int64_t  num_pages;     /* > 0, below 2^31 */
   int32_t  page_size;     /* > 0 */
-  int32_t  num_rows;      /* > 0 */
+  int32_t  num_rows;      /* in [1, 2^22] */
   int32_t  bt_stride;     /* > 0; bt_stride * page_size below 2^31 */
   int32_t  reserved;      /* set to 0 */
 } topkv_page_owner_t;
@@ -724,9 +725,9 @@ typedef struct topkv_page_owner {
  * pages, and before the destination is read or written.  result + 1 serves as
  * topkv_copy_pages' count.  None of the calls allocates or synchronises; all
  * can be captured.  Calls on one owner have to be ordered (one stream).
- * TOPKV_ERR_INVALID_ARG for a bad descriptor, null pointers, a negative or
- * (above num_rows or TOPKV_MAX_BATCH_REQS) too large number of rows, too few
- * pairs or a short or misaligned workspace. */
+ * TOPKV_ERR_INVALID_ARG for a bad descriptor, null pointers, a negative
+ * number of rows or one above TOPKV_MAX_BATCH_REQS (fork, grow: or num_rows),
+ * too few pairs or a short or misaligned workspace. */
 
 /* Workspace bytes of fork, grow and compact for this owner (16-byte aligned
  * device memory, scratch); -1 for a bad descriptor. */
@@ -793,7 +794,9 @@ topkv_status_t topkv_pages_compact(const topkv_page_owner_t* owner, int32_t* pai
  *              [0, max_pairs]), or NULL for all
  * TOPKV_ERR_INVALID_ARG for bad or different geometries, a layer range
  * outside a pool, null pairs or a negative max_pairs; max_pairs == 0 or
- * num_layers == 0 launches nothing.  One kernel; does not synchronise. */
+ * num_layers == 0 launches nothing.  TOPKV_ERR_UNSUPPORTED where max_pairs
+ * times the page's tiles (of up to 32 KiB) reach 2^31, or for more than 65535
+ * layers.  One kernel; does not synchronise. */
 topkv_status_t topkv_copy_pages(const topkv_pool_t* src, const topkv_pool_t* dst, int32_t first_layer,
                                 int32_t num_layers, const int32_t* pairs, int32_t max_pairs,
                                 const int32_t* count, hipStream_t stream);

@@ -36,6 +36,7 @@ struct Args {
   bool out_wide;              // rows of out on 16-byte addresses
 };
 
+constexpr int64_t kMostGroups = 1 << 23;   // workgroups of up to 512 threads in a launch of fewer than 2^32 threads
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kLog2e = 1.44269504088896341f;
 

@@ -28,7 +28,7 @@ __device__ __forceinline__ void store(void* p, int64_t i, float v) {
 // what geometries run that the matrix-unit kernels do not take.
 template <int QT, int KT, int NR>
 __global__ __launch_bounds__(64 * kWaves) void kv_attention_general_kernel(Args a) {
-  const int64_t row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kWaves + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= (int64_t)a.total_q * a.num_heads) return;
   const int32_t token = (int32_t)(row / a.num_heads), head = (int32_t)(row - (int64_t)token * a.num_heads);
@@ -94,8 +94,9 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_general_kernel(Args 
 
 template <int QT, int KT>
 void launch_general(const Args& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.total_q * a.num_heads;
-  const dim3 grid((unsigned)((rows + kWaves - 1) / kWaves));
+  const int64_t groups = ((int64_t)a.total_q * a.num_heads + kWaves - 1) / kWaves;
+  const int64_t wide = groups < kMostGroups ? groups : kMostGroups;
+  const dim3 grid((unsigned)wide, (unsigned)((groups + wide - 1) / wide));
   if (a.head_dim <= 256)
     hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_general_kernel<QT, KT, 4>), grid, dim3(64 * kWaves), 0, stream, a);
   else

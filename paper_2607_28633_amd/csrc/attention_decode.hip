@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
       }
       float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                         fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-      top = max_quarters(top) * a.scale;
+      top = max_quarters(top) * a.scale - lift<T>(0.f);
       if (__any(top > m)) {                                      // some row's maximum rises
         const float up = fmaxf(m, top), fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
         m = up;
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
         for (int i = 0; i < 4; ++i) {
           const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], a.scale, -base));
           l += w;
-          p[b * 4 + i] = (typename Elem<T>::type)w;              // in [0, 1]: rounded for the matrix units, its sum is not
+          p[b * 4 + i] = (typename Elem<T>::type)w;              // rounded for the matrix units, its sum is not
         }
       // values by columns: lane (d, quad) takes keys 4 quad .. + 3 of each half, as the weights lie
       const char* values = tile + (kLatent ? 0 : kKeyBytes);
@@ -326,7 +326,7 @@ bool decode_takes(const Args& a) {
   const bool latent = a.value_bytes == 0;
   if (!rows_aligned(a) || a.head_dim > (latent ? 128 : 256)) return false;
   const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
-  return items * units(a) <= INT32_MAX && (int64_t)wanted_shares(a) * a.num_heads <= INT32_MAX;
+  return items * units(a) <= kMostGroups && (int64_t)wanted_shares(a) * a.num_heads <= kMostGroups;
 }
 
 int64_t decode_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }

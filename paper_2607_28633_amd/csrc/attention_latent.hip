@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
         for (int i = 0; i < 4; ++i)
           if (!(there >> (key_half * 16 + quad * 4 + i) & 1)) x[i] = -INFINITY;
       }
-      const float top = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale;
+      const float top = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale - lift<T>(kSlack);
       if (quad == 0) s_top[key_half][row_block * 16 + row] = top;
     }
     __syncthreads();
@@ -342,7 +342,7 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
 bool latent_takes(const Args& a) {
   if (!rows_aligned(a) || a.value_bytes != 0 || a.head_dim <= 128 || a.head_dim > KD || a.value_dim > VD) return false;
   const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
-  return items * units(a) <= INT32_MAX && (int64_t)wanted_shares(a) * a.num_heads <= INT32_MAX;
+  return items * units(a) <= kMostGroups && (int64_t)wanted_shares(a) * a.num_heads <= kMostGroups;
 }
 
 int64_t latent_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }

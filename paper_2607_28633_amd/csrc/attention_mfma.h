@@ -52,6 +52,11 @@ template <> struct Elem<TOPKV_FP16> {
   }
 };
 
+// Weights are exp2(score - reference).  Half floats lose what lies below 2^-14, which a long cache's many small weights
+// may be together: their reference lies this far (in powers of two) below the largest score, so that the largest weight
+// is 2^14, or 2^6 where the reference may fall 2^8 behind.
+template <int T> constexpr float lift(float slack) { return T == TOPKV_FP16 ? 14.f - slack : 0.f; }
+
 // Eight e4m3 values as eight of T.
 template <int T>
 __device__ __forceinline__ uint4v widen(uint2v w) {

@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
-      top = max_halves(top) * a.scale;
+      top = max_halves(top) * a.scale - lift<T>(kSlack);
       if (__any(top > m + kSlack)) {                             // some row's scores left the maximum behind
         const float up = fmaxf(m, top), fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
         m = up;
@@ -703,7 +703,7 @@ bool prompt_takes(const Args& a) {
   if (a.value_bytes == 0 || a.head_dim % 8 != 0 || a.head_dim > 256) return false;
   if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
   const int64_t items = most_tiles(a, kFew) > wanted_shares(a) ? most_tiles(a, kFew) : wanted_shares(a);
-  return items * a.kv_heads <= INT32_MAX;
+  return items * a.kv_heads <= kMostGroups;
 }
 
 int64_t prompt_workspace(const Args& a) {

@@ -856,20 +856,28 @@ def _token_stride(t: torch.Tensor) -> int:
     T, H, D = t.shape
     if t.numel() and ((D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D)):
         raise ValueError("a token's heads must be contiguous (any stride between tokens)")
-    return max(int(t.stride(0)), H * D) if T > 1 else H * D
+    return max(int(t.stride(0)), H * D) if T > 1 else H * D      # one token: no stride to go by
 
 
-def _rows_ptr(x) -> int:
-    """Device address of a [tokens][heads][dim] tensor with any stride between tokens (or an address)."""
-    if isinstance(x, torch.Tensor):
-        if not x.is_cuda and x.numel():
-            raise ValueError("tensor arguments must live in device memory")
-        if x.dim() == 3:
-            if x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2]:
-                raise ValueError("tokens must not overlap")
-            _token_stride(x)
-            return x.data_ptr()
-    return _ptr(x)
+def _rows_ptr(x, tokens, heads, dim, stride, dtype) -> int:
+    """Device address of a [tokens][heads][dim] tensor that is as the options say (or an address)."""
+    if not isinstance(x, torch.Tensor):
+        return _ptr(x)
+    if not x.is_cuda and x.numel():
+        raise ValueError("tensor arguments must live in device memory")
+    if x.dim() != 3 or x.shape[0] < tokens or x.shape[1] != heads or x.shape[2] != dim:
+        raise ValueError(f"expected a [{tokens} or more][{heads}][{dim}] tensor, got {list(x.shape)}")
+    if _DTYPE.get(x.dtype) != dtype:
+        raise ValueError("the tensor's type is not the options'")
+    if x.shape[0] > 1 and x.numel() and (_token_stride(x) != stride or x.stride(0) < heads * dim):
+        raise ValueError("the stride between tokens is not the options'")
+    _token_stride(x)
+    return x.data_ptr()
+
+
+def _query_ptrs(cache, attn, q, out, tokens):
+    return (_P(_rows_ptr(q, tokens, attn.num_heads, cache.pool.head_dim, attn.q_stride, attn.dtype)),
+            _P(_rows_ptr(out, tokens, attn.num_heads, attn.value_dim, attn.out_stride, attn.dtype)))
 
 
 def attention_options(q, out, *, kv_heads, scale, kv_dtype=None, window=0, sinks=0, k_scale=1.0,
@@ -888,9 +896,9 @@ def attention_options(q, out, *, kv_heads, scale, kv_dtype=None, window=0, sinks
                              float(scale), float(k_scale), float(v_scale), 0.0, _token_stride(q), _token_stride(out))
 
 
-def _lse_ptr(t) -> int:
-    if isinstance(t, torch.Tensor) and t.dtype != torch.float32:
-        raise ValueError("lse must be float32")
+def _lse_ptr(t, tokens, heads) -> int:
+    if isinstance(t, torch.Tensor) and (t.dtype != torch.float32 or t.numel() < tokens * heads):
+        raise ValueError("lse must be float32 [tokens][heads]")
     return _ptr(t)
 
 
@@ -904,8 +912,9 @@ def topkv_attention_workspace_bytes(cache: topkv_view_t, attn: topkv_attention_t
 def prepare_attention_decode(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q, out, workspace=None,
                              lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
     wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
-    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)), _P(_rows_ptr(q)),
-            _P(_rows_ptr(out)), _P(_lse_ptr(lse)), _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
+    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)),
+            *_query_ptrs(cache, attn, q, out, int(num_reqs)), _P(_lse_ptr(lse, int(num_reqs), attn.num_heads)),
+            _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
     return PreparedCall("topkv_attention_decode", args, (cache, attn))
 
 
@@ -913,8 +922,8 @@ def prepare_attention_prompt(cache: topkv_view_t, attn: topkv_attention_t, num_r
                              workspace=None, lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
     wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
     args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)),
-            _P(_table_ptr(q_starts)), _I32(int(total_q)), _P(_rows_ptr(q)), _P(_rows_ptr(out)), _P(_lse_ptr(lse)),
-            _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
+            _P(_table_ptr(q_starts)), _I32(int(total_q)), *_query_ptrs(cache, attn, q, out, int(total_q)),
+            _P(_lse_ptr(lse, int(total_q), attn.num_heads)), _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
     return PreparedCall("topkv_attention_prompt", args, (cache, attn))
 
 

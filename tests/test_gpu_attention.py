@@ -306,6 +306,77 @@ def test_prompt_tokens_to_come_do_not_reach_back(tk, kw, junk):
     assert all(not torch.isfinite(c.out_d[t, h]).all() for t, h in bad)
 
 
+@pytest.mark.parametrize("decode", [True, False])
+def test_many_small_weights(tk, decode):
+    """One key far above 40000 others whose weights are each below half floats' normal numbers: together they count."""
+    say("[attention] many small weights")
+    n = 40001
+    c = Case(41, [n], None if decode else [3], q_type=FP, kv_type=FP, kv=1, group=4, dim=64, page=64)
+    c.q[:] = 0
+    c.q[..., 0] = 8.0
+    keys = c.pool[:, 0]
+    keys[..., 0] = 0.0
+    first = int(c.tables[0, 0])
+    keys[first, 5, :, 0] = 10.375                                    # e^(8 * 10.375 / 8): each other weight is 3.1e-5
+    c.pool[:, 1][..., ::2] = c.pool[:, 1][..., ::2].abs()
+    c.device(tk)
+    c.call(tk)
+    c.check()
+
+
+@pytest.mark.parametrize("which", ["cache", "q", "out", "all"])
+@pytest.mark.parametrize("kw", [dict(), dict(kv_type=F8), dict(planes=1, kv=1, group=5, dim=576, value=512)])
+def test_odd_addresses(tk, which, kw):
+    """Pools, queries and outputs that start off 16-byte addresses."""
+    say(f"[attention] {which} off alignment {kw}")
+    for news in (None, [60, 5, 0]):
+        c = Case(43, [300, 5, 90], news, **kw).device(tk)
+
+        def moved(t):
+            flat = torch.empty(t.untyped_storage().nbytes() + 64, dtype=torch.uint8, device="cuda")
+            at = flat[2 if t.element_size() == 2 else 1:][:t.untyped_storage().nbytes()]
+            at.copy_(torch.empty(0, dtype=torch.uint8, device="cuda").set_(t.untyped_storage()))
+            c.keep = getattr(c, "keep", []) + [flat]
+            return at.data_ptr()
+
+        pool = c.pool_d
+        if which in ("cache", "all"):
+            c.cache.pool.base = moved(c.pool_d)
+        q = moved(c.q_d) if which in ("q", "all") else c.q_d
+        out, kept = c.out_d, c.out_full
+        if which in ("out", "all"):
+            flat = torch.full((kept.numel() + 8,), 77.0, dtype=kept.dtype, device="cuda")
+            c.out_full = flat[1:1 + kept.numel()].view(kept.shape)
+            c.out_d = c.out_full.unflatten(1, out.shape[1:])
+        c.q_d = q
+        if news is None:
+            tk.topkv_attention_decode(c.cache, c.options, 3, c.lens_d, q, c.out_d.data_ptr(), c.work, lse=c.lse_d)
+        else:
+            tk.topkv_attention_prompt(c.cache, c.options, 3, c.lens_d, c.starts_d, c.total, q, c.out_d.data_ptr(), c.work,
+                                      lse=c.lse_d)
+        c.check()
+        assert pool is c.pool_d
+
+
+def test_tensors_are_looked_over(tk):
+    """The binding refuses tensors that are not what the options describe."""
+    c = Case(47, [30, 40]).device(tk)
+    n, h, d = 2, 8, 128
+    good = dict(q=c.q_d, out=c.out_d, lse=c.lse_d)
+    for bad in (dict(q=c.q_d[:1]), dict(q=c.q_d[:, :4]), dict(q=c.q_d.half()), dict(q=c.q_d.cpu()),
+                dict(out=torch.empty((n, h, 64), dtype=BF, device="cuda")), dict(q=torch.empty((n, 2 * h, d), dtype=BF, device="cuda")[:, ::2]),
+                dict(q=torch.empty((n, 3 * h, d), dtype=BF, device="cuda")[:, :h]), dict(q=c.q_d[:1].expand(n, h, d)),
+                dict(lse=torch.empty((n, h), dtype=torch.float64, device="cuda")), dict(lse=c.lse_d[:1]),
+                dict(out=c.out_d.transpose(1, 2).contiguous().transpose(1, 2))):
+        a = {**good, **bad}
+        with pytest.raises(ValueError):
+            tk.topkv_attention_decode(c.cache, c.options, n, c.lens_d, a["q"], a["out"], c.work, lse=a["lse"])
+    with pytest.raises(ValueError):
+        tk.attention_options(c.q_d, c.out_d.float(), kv_heads=2, scale=1.0)
+    with pytest.raises(ValueError):
+        tk.attention_options(c.q_d, c.out_d[:2], kv_heads=2, scale=1.0, kv_dtype=torch.int8)
+
+
 def test_lse_is_optional(tk):
     for news in (None, [30, 5]):
         c = Case(3, [300, 5], news).device(tk)
