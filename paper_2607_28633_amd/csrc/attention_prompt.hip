@@ -157,10 +157,11 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
     cutting = pays<kWaves, KD>(a);
     if (cutting && number >= plan.shares) return;
   }
+  Rows mine;
   const auto weight = [&](int32_t r) -> int64_t {
-    const Rows w = rows_of(a, r);
-    const int32_t n = w.tiles<kRows>(a);
-    return cutting && n > 0 ? (int64_t)n * w.depth<kRows>(a) : n;
+    mine = rows_of(a, r);
+    const int32_t n = mine.tiles<kRows>(a);
+    return cutting && n > 0 ? (int64_t)n * mine.depth<kRows>(a) : n;
   };
   if (threadIdx.x == 0) s_request = -1;
   Scan<int64_t> scan = scan_requests<int64_t, kWaves>(a.num_reqs, weight);
@@ -176,15 +177,15 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
     upto = at + 1;
   }
   if (at >= 0 && scan.holds(at)) {
-    s_request = scan.find(at, weight);
+    s_request = scan.lo + 1 < scan.hi ? scan.find(at, weight) : scan.lo;   // the thread's only request is still in hand
     s_base = scan.base;
-    s_rows = rows_of(a, s_request);
+    s_rows = mine;
   }
   __syncthreads();
   int32_t request = __builtin_amdgcn_readfirstlane(s_request);
   if (request < 0) return;
   int64_t base = s_base;
-  Rows mine = s_rows;
+  mine = s_rows;
 
   const char* cache = a.cache + (int64_t)kv_head * a.head_bytes;
   const int32_t chunks = a.head_dim / 8;
@@ -416,18 +417,31 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
       }
       const bool clear = there == ~0ull && open(first, wave_first, wave_last);
       if (!clear) {
-        const int32_t low = a.window > 0 ? pos - a.window : -1, behind = span.start - span.head;
+        if (there != ~0ull) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint32_t is = (uint32_t)(there >> (b * 32)) >> (half * 4);
+          for (int b = 0; b < 2; ++b) {
+            const uint32_t is = (uint32_t)(there >> (b * 32)) >> (half * 4);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int32_t k = first + b * 32 + (i >> 2) * 8 + half * 4 + (i & 3);
-            const int32_t j = k < span.head ? k : k + behind;
-            const bool seen = (is >> ((i >> 2) * 8 + (i & 3)) & 1) & (j <= pos) & ((j > low) | (j < a.sinks));
-            x[b][i] = seen ? x[b][i] : -INFINITY;
+            for (int i = 0; i < 16; ++i) x[b][i] = is >> ((i >> 2) * 8 + (i & 3)) & 1 ? x[b][i] : -INFINITY;
           }
         }
+        // The row sees key numbers below `few` (first tokens) and `wide` ones from `from` on, here counted from the lane's
+        // first key of the tile: two comparisons a key.
+        const int32_t here = first + half * 4, behind = span.head - span.start;
+        const int32_t last = pos + behind, from = (a.window > 0 ? last - a.window + 1 : 0) - here;
+        const int32_t few = (a.sinks + behind < last + 1 ? a.sinks + behind : last + 1) > span.head
+                                ? (a.sinks + behind < last + 1 ? a.sinks + behind : last + 1) - here
+                                : span.head - here;
+        const uint32_t wide = pos < 0 ? 0u : (uint32_t)(last + 1 - here - from);
+        const int32_t firsts = pos < 0 ? INT32_MIN : few;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int32_t k = b * 32 + (i >> 2) * 8 + (i & 3);
+            const bool seen = (k < firsts) | ((uint32_t)(k - from) < wide);
+            x[b][i] = seen ? x[b][i] : -INFINITY;
+          }
       }
       float top = -INFINITY;
 #pragma unroll
