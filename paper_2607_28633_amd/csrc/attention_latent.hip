@@ -6,11 +6,12 @@
 // and the row is read from memory once for all: 2 * 64 * (576 + 512) flops
 // for 1152 bytes, still less than the matrix units do in the time the bytes
 // take.  The output, 64 rows of 512, is too much for one wave: the eight waves
-// of a workgroup share a tile of 32 keys.  For the scores a wave takes 16 keys
-// and 16 rows, for the output 64 elements of all rows; in between the weights
-// go through LDS.  Three tiles are in LDS, one in use and two on their way
-// straight from memory, which is what keeps the bytes coming: a CU holds one
-// workgroup.  Three barriers a tile cost little against the tile's bytes.
+// of a workgroup share a tile of 32 keys.  For the scores a wave takes 16 keys,
+// 16 rows and, where there are few rows, a half or a quarter of the elements;
+// the parts meet in LDS, from where every wave makes all weights for itself and
+// multiplies them with its 64 elements of the values.  Three tiles are in LDS,
+// one in use and two on their way straight from memory, which is what keeps
+// the bytes coming: a CU holds one workgroup.
 #include <type_traits>
 
 #include "attention_internal.h"
@@ -37,11 +38,13 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
   typedef typename Elem<T>::type elem;
   constexpr int kRows = 16 * RB;
   __shared__ __attribute__((aligned(16))) char s_tile[kBuffers][kTileBytes];
-  __shared__ __attribute__((aligned(16))) elem s_weight[kRows][kTile];
-  __shared__ float s_top[2][kRows], s_sum[2][kRows];
+  constexpr int kParts = 4 / RB;                                 // of the elements, in the first product
+  constexpr int kSteps = (KD / 32 + kParts - 1) / kParts;        // of 32 elements, in a part
+  constexpr int kPitch = kTile + 4;                              // floats of a row of scores: rows start 4 banks apart
+  __shared__ __attribute__((aligned(16))) float s_score[kParts][kRows][kPitch];
 
   const int wave = threadIdx.x >> 6;
-  const int key_half = wave & 1, row_block = wave >> 1;          // the wave's scores; none where row_block >= RB
+  const int key_half = wave & 1, row_block = (wave >> 1) % RB, part = (wave >> 1) / RB;   // of the wave's scores
   const int32_t groups = (a.group + kRows - 1) / kRows;
   const int32_t units = a.kv_heads * groups, eight = blockIdx.x / (8 * units), within = blockIdx.x - eight * 8 * units;
   const int32_t share = eight * 8 + (within & 7), sub = within >> 3;   // over the XCDs as in attention_decode.hip
@@ -116,6 +119,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
             cache + (int64_t)((uint64_t)(uint32_t)__shfl(hi, r, 64) << 32 | (uint32_t)__shfl(lo, r, 64)) + c * kChunkBytes;
         if (c < chunks) {
           if constexpr (kF8) raw[i] = *reinterpret_cast<const uint2v*>(from);
+          else if constexpr (kCut) load_once_to_lds(s_tile[buf] + piece * 1024, from);
           else load_to_lds(s_tile[buf] + piece * 1024, from);
         }
       }
@@ -153,28 +157,29 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
   there1 = (uint32_t)__ballot(off >= 0);
   if (begin + kTile < end) fetch(1, off);
 
-  vec8 q[KD / 32];
+  vec8 q[kSteps];
   {
     const int32_t h = first_row + row_block * 16 + row;
     const char* from =
         static_cast<const char*>(a.q) + ((int64_t)request * a.q_stride + (int64_t)(kv_head * a.group + h) * a.head_dim) * 2;
 #pragma unroll
-    for (int s = 0; s < KD / 32; ++s) {
-      const int d = s * 32 + quad * 8;
+    for (int s = 0; s < kSteps; ++s) {
+      const int d = (s * kParts + part) * 32 + quad * 8;
       union {
         uint4v w;
         vec8 v;
       } u;
       u.w = uint4v{0, 0, 0, 0};
-      if (row_block < RB && h < a.group && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(from + 2 * d);
+      if (h < a.group && d < a.head_dim) u.w = *reinterpret_cast<const uint4v*>(from + 2 * d);
       q[s] = u.v;
     }
   }
   float4v acc[RB][4];
-  float m[RB], l = 0.f;
+  float m[RB], l[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     m[b] = -INFINITY;
+    l[b] = 0.f;
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[b][t] = float4v{0.f, 0.f, 0.f, 0.f};
   }
@@ -189,7 +194,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
       else wait_loads();
       settle(buf, there);
     }
-    __syncthreads();                                             // the tile is whole; the one before it is done with
+    __syncthreads();                                             // the tile is whole; the one before it and its scores are done with
     if constexpr (kF8) {
       if (first + kTile < end) settle(next, there1);
     }
@@ -203,58 +208,55 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     int here = lane;
     asm volatile("" : "+v"(here));                               // and these in the tile's loop
     const int row = here & 15, quad = here >> 4;
-    float4v x = {0.f, 0.f, 0.f, 0.f};
-    if (row_block < RB) {
+    {
+      float4v x = {0.f, 0.f, 0.f, 0.f};
       const int r = key_half * 16 + row;
 #pragma unroll
-      for (int s = 0; s < KD / 32; ++s) {
-        const vec8 k = *reinterpret_cast<const vec8*>(tile + (r * NC + ((s * 4 + quad) ^ swizzle<NC>(r))) * 16);
+      for (int s = 0; s < kSteps; ++s) {
+        const int n = s * kParts + part;
+        if (kSteps * kParts > KD / 32 && n >= KD / 32) break;    // the last part is a step short
+        const vec8 k = *reinterpret_cast<const vec8*>(tile + (r * NC + ((n * 4 + quad) ^ swizzle<NC>(r))) * 16);
         x = Elem<T>::mfma16(k, q[s], x);
+      }
+      *reinterpret_cast<float4v*>(&s_score[part][row_block * 16 + row][key_half * 16 + quad * 4]) = x;
+    }
+    __syncthreads();
+    // lane (row, quad) takes keys 8 quad .. + 7 of its row: the layout the second product wants
+    vec8 p[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        float4v sum = *reinterpret_cast<const float4v*>(&s_score[0][b * 16 + row][quad * 8 + e]);
+#pragma unroll
+        for (int n = 1; n < kParts; ++n) sum += *reinterpret_cast<const float4v*>(&s_score[n][b * 16 + row][quad * 8 + e]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[e + i] = sum[i];
       }
       if (there != ~0u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(there >> (key_half * 16 + quad * 4 + i) & 1)) x[i] = -INFINITY;
+        for (int i = 0; i < 8; ++i) x[i] = there >> (quad * 8 + i) & 1 ? x[i] : -INFINITY;
       }
-      const float top = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale - lift<T>(kSlack);
-      if (quad == 0) s_top[key_half][row_block * 16 + row] = top;
-    }
-    __syncthreads();
-    float fall_mine = 1.f, base_mine = 0.f;
+      float top = x[0];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {                               // every wave keeps every row's maximum
-      const float top = fmaxf(s_top[0][b * 16 + row], s_top[1][b * 16 + row]);
-      float fall = 1.f;
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+      top = max_quarters(top) * a.scale - lift<T>(kSlack);
       if (__any(top > m[b] + kSlack)) {
-        const float up = fmaxf(m[b], top);
-        fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
+        const float up = fmaxf(m[b], top), fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
         m[b] = up;
+        l[b] *= fall;
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[b][t] *= fall;
       }
-      if (b == row_block) {
-        fall_mine = fall;
-        base_mine = m[b] == -INFINITY ? 0.f : m[b];
+      const float base = m[b] == -INFINITY ? 0.f : m[b];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base));
+        l[b] += w;
+        p[b][i] = (elem)w;                                       // rounded for the matrix units, its sum is not
       }
     }
-    if (row_block < RB) {
-      l *= fall_mine;
-      union {
-        elem e[4];
-        uint2v w;
-      } u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base_mine));
-        l += w;
-        u.e[i] = (elem)w;                                        // rounded for the matrix units, its sum is not
-      }
-      *reinterpret_cast<uint2v*>(&s_weight[row_block * 16 + row][key_half * 16 + quad * 4]) = u.w;
-    }
-    __syncthreads();
-    vec8 p[RB];
-#pragma unroll
-    for (int b = 0; b < RB; ++b) p[b] = *reinterpret_cast<const vec8*>(&s_weight[b * 16 + row][quad * 8]);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {                                // 16 elements of the value at a time, by columns
       union {
@@ -274,17 +276,11 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     buf = next;
   }
 
-  // sums of the two halves of the keys
-  if (row_block < RB) {
-    l = sum_quarters(l);
-    if (quad == 0) s_sum[key_half][row_block * 16 + row] = l;
-  }
-  __syncthreads();
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const int32_t h = first_row + b * 16 + row, head = kv_head * a.group + h;
+    const float sum = sum_quarters(l[b]);
     if (h >= a.group) continue;
-    const float sum = s_sum[0][b * 16 + row] + s_sum[1][b * 16 + row];
     const int64_t slot = (2 * (int64_t)share + opens) * a.num_heads + head;
     const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
 #pragma unroll
@@ -305,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
         a.lse[(int64_t)request * a.num_heads + head] = sum == 0.f ? -INFINITY : (m[b] + __builtin_amdgcn_logf(sum)) * kLn2;
     }
   }
-  __syncthreads();                                               // tiles and sums are free again
+  __syncthreads();                                               // tiles and scores are free again
   }
 }
 

@@ -122,6 +122,11 @@ __device__ __forceinline__ void load_to_lds(char* lds, const char* from) {
   const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(L)lds);
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
 }
+__device__ __forceinline__ void load_once_to_lds(char* lds, const char* from) {     // not kept in the L2
+  typedef char __attribute__((address_space(3))) * L;
+  const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(L)lds);
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
