@@ -8,8 +8,8 @@
 // take.  The output, 64 rows of 512, is too much for one wave: the eight waves
 // of a workgroup share a tile of 32 keys.  For the scores a wave takes 16 keys,
 // 16 rows and, where there are few rows, a half or a quarter of the elements;
-// the parts meet in LDS, from where every wave makes all weights for itself and
-// multiplies them with its 64 elements of the values.  Three tiles are in LDS,
+// the parts meet in LDS, from where the weights come that a wave multiplies with
+// its 64 elements of the values.  Three tiles are in LDS,
 // one in use and two on their way straight from memory, which is what keeps
 // the bytes coming: a CU holds one workgroup.
 #include <type_traits>
@@ -41,7 +41,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
   constexpr int kParts = 4 / RB;                                 // of the elements, in the first product
   constexpr int kSteps = (KD / 32 + kParts - 1) / kParts;        // of 32 elements, in a part
   constexpr int kPitch = kTile + 4;                              // floats of a row of scores: rows start 4 banks apart
-  __shared__ __attribute__((aligned(16))) float s_score[kParts][kRows][kPitch];
+  constexpr bool kEach = RB < 4;                                 // every wave makes all weights, or each wave its own for all
+  __shared__ __attribute__((aligned(16))) float s_score[kEach ? kParts : 1][kEach ? kRows : 1][kPitch];
+  __shared__ __attribute__((aligned(16))) elem s_weight[kEach ? 1 : kRows][kTile];
+  __shared__ float s_top[2][kEach ? 1 : kRows], s_sum[2][kEach ? 1 : kRows];
 
   const int wave = threadIdx.x >> 6;
   const int key_half = wave & 1, row_block = (wave >> 1) % RB, part = (wave >> 1) / RB;   // of the wave's scores
@@ -208,8 +211,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     int here = lane;
     asm volatile("" : "+v"(here));                               // and these in the tile's loop
     const int row = here & 15, quad = here >> 4;
+    float4v x = {0.f, 0.f, 0.f, 0.f};
     {
-      float4v x = {0.f, 0.f, 0.f, 0.f};
       const int r = key_half * 16 + row;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
@@ -218,29 +221,30 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
         const vec8 k = *reinterpret_cast<const vec8*>(tile + (r * NC + ((n * 4 + quad) ^ swizzle<NC>(r))) * 16);
         x = Elem<T>::mfma16(k, q[s], x);
       }
-      *reinterpret_cast<float4v*>(&s_score[part][row_block * 16 + row][key_half * 16 + quad * 4]) = x;
     }
+    vec8 p[RB];
+    if constexpr (kEach) {
+    *reinterpret_cast<float4v*>(&s_score[part][row_block * 16 + row][key_half * 16 + quad * 4]) = x;
     __syncthreads();
     // lane (row, quad) takes keys 8 quad .. + 7 of its row: the layout the second product wants
-    vec8 p[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      float x[8];
+      float y[8];
 #pragma unroll
       for (int e = 0; e < 8; e += 4) {
         float4v sum = *reinterpret_cast<const float4v*>(&s_score[0][b * 16 + row][quad * 8 + e]);
 #pragma unroll
         for (int n = 1; n < kParts; ++n) sum += *reinterpret_cast<const float4v*>(&s_score[n][b * 16 + row][quad * 8 + e]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[e + i] = sum[i];
+        for (int i = 0; i < 4; ++i) y[e + i] = sum[i];
       }
       if (there != ~0u) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = there >> (quad * 8 + i) & 1 ? x[i] : -INFINITY;
+        for (int i = 0; i < 8; ++i) y[i] = there >> (quad * 8 + i) & 1 ? y[i] : -INFINITY;
       }
-      float top = x[0];
+      float top = y[0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
       top = max_quarters(top) * a.scale - lift<T>(kSlack);
       if (__any(top > m[b] + kSlack)) {
         const float up = fmaxf(m[b], top), fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
@@ -252,10 +256,52 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
       const float base = m[b] == -INFINITY ? 0.f : m[b];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base));
+        const float w = __builtin_amdgcn_exp2f(fmaf(y[i], a.scale, -base));
         l[b] += w;
         p[b][i] = (elem)w;                                       // rounded for the matrix units, its sum is not
       }
+    }
+    } else {
+    // 64 rows: making all weights eight times over costs more than two exchanges (64 heads 109 us, 95 so; 16 heads 58, 64 so)
+    if (there != ~0u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = there >> (key_half * 16 + quad * 4 + i) & 1 ? x[i] : -INFINITY;
+    }
+    const float best = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale - lift<T>(kSlack);
+    if (quad == 0) s_top[key_half][row_block * 16 + row] = best;
+    __syncthreads();
+    float fall_mine = 1.f, base_mine = 0.f;
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {                               // every wave keeps every row's maximum
+      const float top = fmaxf(s_top[0][b * 16 + row], s_top[1][b * 16 + row]);
+      float fall = 1.f;
+      if (__any(top > m[b] + kSlack)) {
+        const float up = fmaxf(m[b], top);
+        fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
+        m[b] = up;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[b][t] *= fall;
+      }
+      if (b == row_block) {
+        fall_mine = fall;
+        base_mine = m[b] == -INFINITY ? 0.f : m[b];
+      }
+    }
+    l[0] *= fall_mine;                                           // of the wave's own rows and keys
+    union {
+      elem e[4];
+      uint2v w;
+    } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base_mine));
+      l[0] += w;
+      u.e[i] = (elem)w;
+    }
+    *reinterpret_cast<uint2v*>(&s_weight[row_block * 16 + row][key_half * 16 + quad * 4]) = u.w;
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < RB; ++b) p[b] = *reinterpret_cast<const vec8*>(&s_weight[b * 16 + row][quad * 8]);
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {                                // 16 elements of the value at a time, by columns
@@ -276,10 +322,17 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     buf = next;
   }
 
+  if constexpr (!kEach) {
+    const float sum = sum_quarters(l[0]);
+    if (quad == 0) s_sum[key_half][row_block * 16 + row] = sum;
+    __syncthreads();
+  }
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const int32_t h = first_row + b * 16 + row, head = kv_head * a.group + h;
-    const float sum = sum_quarters(l[b]);
+    float sum;
+    if constexpr (kEach) sum = sum_quarters(l[b]);
+    else sum = s_sum[0][b * 16 + row] + s_sum[1][b * 16 + row];
     if (h >= a.group) continue;
     const int64_t slot = (2 * (int64_t)share + opens) * a.num_heads + head;
     const float inv = sum == 0.f ? 0.f : a.v_scale / sum;
