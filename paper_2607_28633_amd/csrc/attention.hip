@@ -224,7 +224,7 @@ int64_t topkv_attention_workspace_bytes(const topkv_view_t* cache, const topkv_a
   const int64_t one = topkv_attend::decode_takes(a) ? topkv_attend::decode_workspace(a)
                       : topkv_attend::latent_takes(a) ? topkv_attend::latent_workspace(a)
                                                       : 0;
-  const int64_t many = topkv_attend::prompt_takes(a) ? topkv_attend::prompt_workspace(a) : 0;
+  const int64_t many = topkv_attend::prompt_workspace(a);
   return one > many ? one : many;
 }
 

@@ -330,9 +330,7 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
 
 bool decode_takes(const Args& a) {
   const bool latent = a.value_bytes == 0;
-  if (!rows_aligned(a) || a.head_dim > (latent ? 128 : 256)) return false;
-  const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
-  return items * units(a) <= kMostGroups && (int64_t)wanted_shares(a) * a.num_heads <= kMostGroups;
+  return rows_aligned(a) && a.head_dim <= (latent ? 128 : 256) && launchable(a, wanted_shares(a), units(a));
 }
 
 int64_t decode_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }

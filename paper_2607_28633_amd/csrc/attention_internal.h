@@ -7,7 +7,8 @@
 namespace topkv_attend {
 
 // Whether the geometry (not the pointers) is one the kernel takes, the
-// workspace bytes it wants, and the call.
+// workspace bytes it wants at most for the counts of the call or smaller ones,
+// and the call.
 __attribute__((visibility("hidden"))) bool decode_takes(const Args& a);
 __attribute__((visibility("hidden"))) int64_t decode_workspace(const Args& a);
 __attribute__((visibility("hidden"))) topkv_status_t run_decode(const Args& a, void* workspace, hipStream_t stream);

@@ -389,9 +389,8 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
 }  // namespace
 
 bool latent_takes(const Args& a) {
-  if (!rows_aligned(a) || a.value_bytes != 0 || a.head_dim <= 128 || a.head_dim > KD || a.value_dim > VD) return false;
-  const int64_t items = (wanted_shares(a) > a.num_reqs ? wanted_shares(a) : a.num_reqs) + 8;
-  return items * units(a) <= kMostGroups && (int64_t)wanted_shares(a) * a.num_heads <= kMostGroups;
+  return rows_aligned(a) && a.value_bytes == 0 && a.head_dim > 128 && a.head_dim <= KD && a.value_dim <= VD &&
+         launchable(a, wanted_shares(a), units(a));
 }
 
 int64_t latent_workspace(const Args& a) { return plan_bytes(a, wanted_shares(a)); }

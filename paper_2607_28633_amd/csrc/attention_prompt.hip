@@ -675,11 +675,12 @@ int waves_for(const Args& a) {
 
 // Shares of the work where it may be cut, which the kernel decides by the lengths; 0 where the row tiles are enough for
 // certain (twice as many as fit the GPU at once) or no row can see more keys than two shares should have.
+int32_t most_shares(const Args& a) {
+  const int32_t n = resident(a.head_dim) / a.kv_heads;
+  return most_keys(a) <= 2 * kLeast * kTile ? 0 : n < 1 ? 1 : n;
+}
 int32_t wanted_shares(const Args& a) {
-  const int64_t fit = resident(a.head_dim);
-  if (least_tiles(a, kFew) * a.kv_heads >= 2 * fit || most_keys(a) <= 2 * kLeast * kTile) return 0;
-  const int32_t n = (int32_t)(fit / a.kv_heads);
-  return n < 1 ? 1 : n;
+  return least_tiles(a, kFew) * a.kv_heads >= 2 * resident(a.head_dim) ? 0 : most_shares(a);
 }
 
 int64_t up16(int64_t x) { return (x + 15) / 16 * 16; }
@@ -712,16 +713,19 @@ void launch(const Args& a, const Plan& p, hipStream_t stream) {
 
 }  // namespace
 
-bool prompt_takes(const Args& a) {
+bool prompt_geometry(const Args& a) {
   const int64_t unit = a.kv_dtype == TOPKV_FP8_E4M3 ? 8 : 16;
-  if (a.value_bytes == 0 || a.head_dim % 8 != 0 || a.head_dim > 256) return false;
-  if (a.slot_bytes % unit != 0 || a.head_bytes % unit != 0 || a.page_bytes % unit != 0 || a.value_bytes % unit != 0) return false;
-  const int64_t items = most_tiles(a, kFew) > wanted_shares(a) ? most_tiles(a, kFew) : wanted_shares(a);
-  return items * a.kv_heads <= kMostGroups;
+  return a.value_bytes != 0 && a.head_dim % 8 == 0 && a.head_dim <= 256 && a.slot_bytes % unit == 0 &&
+         a.head_bytes % unit == 0 && a.page_bytes % unit == 0 && a.value_bytes % unit == 0 &&
+         (int64_t)most_shares(a) * a.kv_heads <= kMostGroups;
 }
 
+bool prompt_takes(const Args& a) { return prompt_geometry(a) && most_tiles(a, kFew) * a.kv_heads <= kMostGroups; }
+
+// For any number of tokens: fewer may be cut where more are not.
 int64_t prompt_workspace(const Args& a) {
-  const int64_t shares = wanted_shares(a), rows = 2 * shares * a.kv_heads * kCutRows;
+  if (!prompt_geometry(a)) return 0;
+  const int64_t shares = most_shares(a), rows = 2 * shares * a.kv_heads * kCutRows;
   return up16(rows * a.head_dim * 4) + up16(rows * 8) + shares * 16;
 }
 

@@ -12,8 +12,6 @@ constexpr int kTile = 32;                // keys of a tile
 constexpr int kLeast = 8;                // tiles of a share, at least: smaller pieces cost more to join than they save
 constexpr int kSingle = 512;             // longest visible length that is never cut (one launch, no join)
 
-constexpr int kMostShares = 512;
-
 struct Plan {
   int32_t shares;      // wanted; 0: one per request, whatever its length
   int32_t part_dim;    // value_dim, up to a multiple of 8
@@ -195,6 +193,12 @@ void launch_join(const Args& a, const Plan& p, hipStream_t stream) {
     if (deep) hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<TOPKV_FP16, true>), grid, block, 0, stream, a, p);
     else hipLaunchKernelGGL(HIP_KERNEL_NAME(kv_attention_join_kernel<TOPKV_FP16, false>), grid, block, 0, stream, a, p);
   }
+}
+
+// Whether the grid stays a launch's (whatever num_reqs: a workspace for many requests serves fewer too).
+bool launchable(const Args& a, int32_t shares, int32_t units) {
+  const int64_t items = (shares > TOPKV_MAX_BATCH_REQS ? shares : TOPKV_MAX_BATCH_REQS) + 8;
+  return items * units <= kMostGroups && (int64_t)shares * a.num_heads <= kMostGroups;
 }
 
 // Rows on addresses that the wide loads take.

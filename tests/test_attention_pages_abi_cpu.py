@@ -82,6 +82,22 @@ def test_attention_nothing_to_do(tk):  # noqa: F811
     tk.topkv_attention_prompt(view, opt, 3, 0, 0, 0, 0, 0, 0x10000, workspace_bytes=1 << 40, stream=0)
 
 
+@pytest.mark.parametrize("planes,dim,value", [(2, 64, 64), (2, 128, 128), (2, 256, 256), (1, 576, 512), (1, 64, 48), (2, 25, 25)])
+@pytest.mark.parametrize("window", [0, 100, 4000])
+def test_attention_workspace_serves_smaller_calls(tk, planes, dim, value, window):  # noqa: F811
+    """What suffices for many requests and tokens suffices for fewer."""
+    pool = _pool(tk, planes=planes, head_dim=dim)
+    for heads, kv in ((8, 1), (16, 8), (128, 1)):
+        opt = _options(tk, num_heads=heads, kv_heads=kv, value_dim=value, window=window, q_stride=heads * dim,
+                       out_stride=heads * value)
+        for stride in (4, 3000, 15000):
+            view, most = _view(tk, pool, bt_stride=stride), -1
+            for n in (0, 1, 7, 300, 4096):
+                for total in (n, 3 * n + 100, 200000):
+                    most = max(most, tk.topkv_attention_workspace_bytes(view, opt, n, total))
+                    assert tk.topkv_attention_workspace_bytes(view, opt, 4096, 1 << 20) >= most
+
+
 def _owner(tk, **kw):  # noqa: F811
     g = dict(ref_counts=0x1000, block_tables=0x2000, seq_lens=0x3000, num_pages=100, page_size=16, num_rows=4, bt_stride=8,
              reserved=0)
