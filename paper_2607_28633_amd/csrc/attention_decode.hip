@@ -279,7 +279,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][r] - base);
-      if (s_m[w][r] == -INFINITY) continue;                      // no key, or none that counts
+      if (s_m[w][r] == -INFINITY && s_l[w][r] == 0.f) continue;  // no key, or none that counts (a sum of NaN does)
       sum += f * s_l[w][r];
       o += *reinterpret_cast<const float4v*>(s_tile + w * kWaveBytes + (r * kPad + d) * 4) * f;
     }

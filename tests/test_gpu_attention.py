@@ -307,6 +307,24 @@ def test_prompt_tokens_to_come_do_not_reach_back(tk, kw, junk):
 
 
 @pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("kw", [dict(), dict(kv_type=F8), dict(q_type=FP, kv_type=FP, dim=64), dict(dim=25), dict(window=30, sinks=2),
+                                dict(planes=1, kv=1, group=4, dim=576, value=512),
+                                dict(planes=1, kv=1, group=40, dim=576, value=512)])
+def test_queries_of_nan(tk, decode, kw):
+    """A query with a NaN gives NaN, in requests that are cut too, and nothing to the rows beside it."""
+    say(f"[attention] NaN queries {kw} decode={decode}")
+    c = Case(53, [5000, 40, 1], None if decode else [3, 20, 1], **kw)
+    spoiled = [(0, 1), (c.total - 1, 0)]
+    for t, h in spoiled:
+        c.q[t, h, c.dim // 2] = float("nan")
+    c.device(tk)
+    c.call(tk)
+    c.check({k: w for k, w in c.exact().items() if k not in spoiled})
+    for t, h in spoiled:
+        assert torch.isnan(c.out_d[t, h]).all() and torch.isnan(c.lse_d[t, h])
+
+
+@pytest.mark.parametrize("decode", [True, False])
 def test_many_small_weights(tk, decode):
     """One key far above 40000 others whose weights are each below half floats' normal numbers: together they count."""
     say("[attention] many small weights")
