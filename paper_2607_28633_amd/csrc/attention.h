@@ -88,6 +88,16 @@ __device__ __forceinline__ int64_t row_offset(const Args& a, const int32_t* __re
   return (int64_t)e * a.page_bytes + (int64_t)((uint32_t)j - page * (uint32_t)a.page_size) * a.slot_bytes;
 }
 
+// x * scale - base with the product rounded before the difference, as it was where base was made of it: in one fused
+// step the two differ by half a unit in the product's last place, whole powers of two once scores pass 24 bits.
+__device__ __forceinline__ float exponent_of(float x, float scale, float base) {
+#pragma clang fp contract(off)
+  return x * scale - base;
+}
+__device__ __forceinline__ float weight_of(float x, float scale, float base) {
+  return __builtin_amdgcn_exp2f(exponent_of(x, scale, base));
+}
+
 // One element of a row.
 template <int T> struct Load;
 template <> struct Load<TOPKV_BF16> {

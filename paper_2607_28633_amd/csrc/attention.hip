@@ -71,9 +71,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_general_kernel(Args 
     }
 #pragma unroll
     for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s, 64);
-    x *= a.scale;
-    const float top = fmaxf(m, x), safe = top == -INFINITY ? 0.f : top;
-    const float keep = exp2f(m - safe), p = exp2f(x - safe);
+    const float top = fmaxf(m, x * a.scale), safe = top == -INFINITY ? 0.f : top;
+    const float keep = exp2f(m - safe), p = weight_of(x, a.scale, safe);
     m = top;
     l = l * keep + p;
     const char* v = k + a.value_bytes;

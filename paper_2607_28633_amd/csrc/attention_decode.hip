@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
       }
       float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                         fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-      top = max_quarters(top) * a.scale - lift<T>(0.f);
+      top = reference<T>(max_quarters(top), a.scale, 0.f);
       if (__any(top > m)) {                                      // some row's maximum rises
         const float up = fmaxf(m, top), fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
         m = up;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads, resident(KD) / 256) void kv_attention_dec
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], a.scale, -base));
+          const float w = weight_of(x[b][i], a.scale, base);
           l += w;
           p[b * 4 + i] = (typename Elem<T>::type)w;              // rounded for the matrix units, its sum is not
         }

@@ -245,8 +245,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
       float top = y[0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
-      top = max_quarters(top) * a.scale - lift<T>(kSlack);
-      if (__any(top > m[b] + kSlack)) {
+      top = reference<T>(max_quarters(top), a.scale, kSlack);
+      if (__any(top - m[b] > kSlack)) {
         const float up = fmaxf(m[b], top), fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
         m[b] = up;
         l[b] *= fall;
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
       const float base = m[b] == -INFINITY ? 0.f : m[b];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(y[i], a.scale, -base));
+        const float w = weight_of(y[i], a.scale, base);
         l[b] += w;
         p[b][i] = (elem)w;                                       // rounded for the matrix units, its sum is not
       }
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = there >> (key_half * 16 + quad * 4 + i) & 1 ? x[i] : -INFINITY;
     }
-    const float best = max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))) * a.scale - lift<T>(kSlack);
+    const float best = reference<T>(max_quarters(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))), a.scale, kSlack);
     if (quad == 0) s_top[key_half][row_block * 16 + row] = best;
     __syncthreads();
     float fall_mine = 1.f, base_mine = 0.f;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     for (int b = 0; b < RB; ++b) {                               // every wave keeps every row's maximum
       const float top = fmaxf(s_top[0][b * 16 + row], s_top[1][b * 16 + row]);
       float fall = 1.f;
-      if (__any(top > m[b] + kSlack)) {
+      if (__any(top - m[b] > kSlack)) {
         const float up = fmaxf(m[b], top);
         fall = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - up);
         m[b] = up;
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
     } u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float w = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale, -base_mine));
+      const float w = weight_of(x[i], a.scale, base_mine);
       l[0] += w;
       u.e[i] = (elem)w;
     }

@@ -57,6 +57,17 @@ template <> struct Elem<TOPKV_FP16> {
 // is 2^14, or 2^6 where the reference may fall 2^8 behind.
 template <int T> constexpr float lift(float slack) { return T == TOPKV_FP16 ? 14.f - slack : 0.f; }
 
+// The reference for a largest score x * scale: lowered by the lift, unless floats are so far apart there that it would
+// fall further.  The product is rounded as exponent_of() rounds it.
+template <int T>
+__device__ __forceinline__ float reference(float x, float scale, float slack) {
+#pragma clang fp contract(off)
+  const float top = x * scale;
+  if constexpr (lift<T>(0.f) == 0.f) return top;
+  const float low = top - lift<T>(slack);
+  return top - low > lift<T>(slack) ? top : low;
+}
+
 // Eight e4m3 values as eight of T.
 template <int T>
 __device__ __forceinline__ uint4v widen(uint2v w) {

@@ -325,6 +325,46 @@ def test_queries_of_nan(tk, decode, kw):
 
 
 @pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("kw", [dict(q_type=FP, kv_type=FP), dict(), dict(q_type=FP, kv_type=FP, dim=25),
+                                dict(q_type=FP, kv_type=FP, planes=1, kv=1, group=4, dim=576, value=512),
+                                dict(q_type=FP, kv_type=FP, planes=1, kv=1, group=64, dim=576, value=512),
+                                dict(q_type=FP, kv_type=FP, dim=256), dict(q_type=FP, kv_type=F8, dim=64)])
+def test_scores_past_24_bits(tk, decode, kw):
+    """Scores so large that neighbouring 32-bit floats lie whole powers of two apart.  One key is far above the others: its
+    weight is the only one, and the result its value.  The weight itself is rounded once (h), the result once more (h)."""
+    say(f"[attention] large scores {kw} decode={decode}")
+    lens = [300 + 7 * k for k in range(12)] + [2500, 2501]
+    c = Case(59, lens, None if decode else [2] * len(lens), **kw)
+    c.q[:] = 0
+    c.q[..., 0] = 400.0                                            # with keys of 208 .. 416 and the scale: 2^15 .. 2^41
+    c.scale, top = 1.0, 416.0
+    keys = c.pool[:, 0]
+    keys[..., 0] = torch.nan_to_num(keys[..., 0].float()).clamp(-10, 10).to(c.kv_type)
+    won = []
+    for r, n in enumerate(lens):
+        j = (0, n // 2, n - 2)[r % 3]
+        for i, at in enumerate((j // 3, j)):                       # one that is passed by, and the winner
+            keys[int(c.tables[r, at // c.page]), at % c.page, :, 0] = (208.0, top)[i] if at < j or i else top
+        won.append(j)
+    c.device(tk)
+    for power in range(-2, 25, 2):
+        c.options.scale = 2.0 ** power
+        c.out_full.fill_(77), c.lse_d.fill_(77)
+        c.call(tk)
+        torch.cuda.synchronize()
+        got, lse = c.out_d.double().cpu(), c.lse_d.double().cpu()
+        exact = 2.0 ** power * 400.0 * top * c.k_scale
+        for t in range(c.total):
+            r = t if decode else t // 2
+            at, n = won[r], c.lens[r]
+            row = c.pool[int(c.tables[r, at // c.page]), c.planes - 1, at % c.page].double() * c.v_scale
+            for h in range(c.kv * c.group):
+                v = row[h // c.group][:c.value]
+                assert ((got[t, h] - v).abs() <= 2 * HALF[c.q_type] * v.abs() + TINY[c.q_type]).all(), (power, t, h)
+                assert abs(lse[t, h] - exact) <= 8 * U * exact, (power, t, h)
+
+
+@pytest.mark.parametrize("decode", [True, False])
 def test_many_small_weights(tk, decode):
     """One key far above 40000 others whose weights are each below half floats' normal numbers: together they count."""
     say("[attention] many small weights")
