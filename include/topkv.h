@@ -707,7 +707,7 @@ typedef struct topkv_page_owner {
   int32_t* ref_counts;    /* device int32[num_pages] */
   int32_t* block_tables;  /* device int32[num_rows][bt_stride] */
   int32_t* seq_lens;      /* device int32[num_rows] */
-  int64_t  num_pages;     /* > 0, below 2^31 */
+  int64_t  num_pages;     /* > 0, below 2^31 - 1 */
   int32_t  page_size;     /* > 0 */
   int32_t  num_rows;      /* in [1, 2^22] */
   int32_t  bt_stride;     /* > 0; bt_stride * page_size below 2^31 */
@@ -743,7 +743,8 @@ topkv_status_t topkv_pages_count(const topkv_page_owner_t* owner, int32_t* resul
  * counts fall by one, seq_lens[row] becomes min(seq_lens[row], keep).  A row
  * named twice ends at the smaller length.  Rows outside [0, num_rows), bad
  * lengths, entries outside the pool and entries whose count is 0 already are
- * skipped and counted in result[3] (result[0] TOPKV_ERR_BOUNDS). */
+ * skipped and counted in result[3] (result[0] TOPKV_ERR_BOUNDS); an entry of
+ * -1 is one that was given back already and is passed over. */
 topkv_status_t topkv_pages_free(const topkv_page_owner_t* owner, int32_t num, const int32_t* rows,
                                 const int32_t* keep_lens, int32_t* result, hipStream_t stream);
 
