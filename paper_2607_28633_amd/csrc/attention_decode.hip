@@ -27,8 +27,8 @@ constexpr int kRows = 16;                // query rows of a workgroup
 constexpr int kStep = kTile * kWaves;    // keys of the waves' tiles together
 
 // Shares, by the key width: as many workgroups as 256 CUs hold at once by their LDS (64 KiB at 128 elements, 128 KiB
-// at 256).  131072 tokens, 8 heads of 128: 512 shares 108 us, 768 114, 1024 113, 2048 121; heads of 64, of which four
-// workgroups fit a CU, 512 118 us, 768 123, 1024 131.
+// at 256).  131072 tokens, 8 heads of 128: 512 shares 97 us, 768 102, 1024 103; 262144 tokens, heads of 64, of which four
+// workgroups fit a CU, 512 107 us, 768 112, 1024 105.
 constexpr int resident(int KD) { return KD <= 128 ? 512 : 256; }
 
 // KD, VD: key and value elements of a row, padded; kLatent: the value is the

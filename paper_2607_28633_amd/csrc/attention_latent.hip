@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
       }
     }
     } else {
-    // 64 rows: making all weights eight times over costs more than two exchanges (64 heads 109 us, 95 so; 16 heads 58, 64 so)
+    // 64 rows: making all weights eight times over costs more than two exchanges (64 heads 109 us, 94 so; 16 heads 59, 64 so)
     if (there != ~0u) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = there >> (key_half * 16 + quad * 4 + i) & 1 ? x[i] : -INFINITY;

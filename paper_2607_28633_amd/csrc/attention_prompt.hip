@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   const int wave = threadIdx.x >> 6;
 
   // KV heads side by side: with 8 of them an XCD sees the keys and values of one, which its L2 then serves to all row
-  // tiles (8192 tokens, 8 heads of 128: 1251 us, against 1295 with all heads on every XCD).
+  // tiles (8192 tokens, 8 heads of 128: 1204 us, against 1257 with all heads on every XCD).
   const int32_t number = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - number * a.kv_heads;
   bool cutting = false;                                          // whether this batch is cut: the same for all workgroups
   if constexpr (kCut) {
@@ -677,8 +677,8 @@ int64_t most_keys(const Args& a) {
 }
 
 // Eight waves on one tile halve the loads of a row and have two tiles on their way, four waves twice over a CU start
-// and end more easily.  8192 tokens, heads of 128: 8 waves 1203 us, 4 1292; windows of 128, heads of 64: 250 and 180.
-// Heads of 256 have no registers for more than one wave a SIMD.
+// and end more easily.  8192 tokens, heads of 128: 8 waves 1204 us, 4 1278; windows of 128, heads of 64, in
+// an earlier form: 250 and 180.  Heads of 256 have no registers for more than one wave a SIMD.
 int waves_for(const Args& a) {
   return a.head_dim > 64 && a.head_dim <= 128 && most_keys(a) >= 1024 &&
                  least_tiles(a, kMany) * a.kv_heads >= resident(a.head_dim)

@@ -58,8 +58,8 @@ __device__ Share find_share(const Args& a, int32_t shares, int32_t share) {
 // 16 lanes with 8 elements each for every fourth piece, so that a wave reads
 // whole lines and few of its loads wait for each other; with kDeep, for few
 // requests of many pieces, a workgroup of four waves (1048576 tokens, one KV
-// head, 512 pieces: 119 us with one wave, 109 with four; 64 requests of an
-// e4m3 cache: 163 with one, 184 with eight waves and 64 elements).
+// head, 512 pieces: 107 us with one wave, 96 with four; 64 requests of an
+// e4m3 cache: 155 with one, 157 with four).
 constexpr int kJoinWaves = 4;
 
 template <int T, bool kDeep>
