@@ -364,6 +364,33 @@ def test_scores_past_24_bits(tk, decode, kw):
                 assert abs(lse[t, h] - exact) <= 8 * U * exact, (power, t, h)
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(dim=64), dict(window=200, sinks=3), dict(dim=256, kv=4)])
+def test_large_prompt_scores_past_24_bits(tk, kw):
+    """Whole prompts whose keys grow with their position, by steps of 100 e-folds and more: each token's result is its own
+    value, rounded at most twice."""
+    say(f"[attention] large prompt, large scores {kw}")
+    lens = [1200, 1201]
+    c = Case(61, lens, lens, q_type=FP, kv_type=FP, **{**dict(kv=8, group=8), **kw})
+    c.q[:] = 0
+    c.q[..., 0] = 400.0
+    c.scale = 1.0
+    values = []
+    for r, n in enumerate(lens):
+        at = np.arange(n)
+        page, slot = torch.from_numpy(c.tables[r, at // c.page]).long(), torch.from_numpy(at % c.page)
+        c.pool[page, 0, slot, :, 0] = torch.from_numpy(at).to(FP)[:, None].expand(n, c.kv)       # exact below 2048
+        values.append(c.pool[page, 1, slot])
+    v = torch.cat(values).double().repeat_interleave(c.group, 1)
+    c.device(tk)
+    for power in (-2, 10, 14, 18, 24):
+        c.options.scale = 2.0 ** power
+        c.out_full.fill_(77), c.lse_d.fill_(77)
+        c.call(tk)
+        torch.cuda.synchronize()
+        got = c.out_d[:c.total].double().cpu()
+        assert ((got - v).abs() <= 2 * HALF[FP] * v.abs() + TINY[FP]).all(), power
+
+
 @pytest.mark.parametrize("decode", [True, False])
 def test_many_small_weights(tk, decode):
     """One key far above 40000 others whose weights are each below half floats' normal numbers: together they count."""
