@@ -126,17 +126,19 @@ __device__ __forceinline__ float sum_quarters(float x) {
 // 16 bytes a lane from memory to LDS without registers in between: lane i's go
 // to lds + 16 i (lds the same in all lanes; lanes that are off write nothing).
 // The compiler does not see these loads: wait_loads() before their LDS is read.
+// A scalar write of m0 needs a wait state before a load that takes its LDS
+// address from it, and inside an asm text nobody else puts one there.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"   // that m0 is a register of the target's own is why it is named
 __device__ __forceinline__ void load_to_lds(char* lds, const char* from) {
   typedef char __attribute__((address_space(3))) * L;
   const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(L)lds);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
 }
 __device__ __forceinline__ void load_once_to_lds(char* lds, const char* from) {     // not kept in the L2
   typedef char __attribute__((address_space(3))) * L;
   const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(L)lds);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
