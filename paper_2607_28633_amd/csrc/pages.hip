@@ -356,37 +356,39 @@ __global__ void kv_pages_begin_kernel(int32_t* __restrict__ result) {
 }
 
 // Give back: one workgroup per named row.  The exchange hands each entry to
-// one thread only, so a row named twice gives every page back once.
+// one thread only, so a row named twice gives every page back once.  The other
+// workgroup may lower the row's length at any time: one thread reads it, for all.
 __global__ __launch_bounds__(kThreads) void kv_pages_free_kernel(topkv_page_owner_t o, const int32_t* __restrict__ rows,
                                                                  const int32_t* __restrict__ keep_lens,
                                                                  int32_t* __restrict__ result) {
+  __shared__ int32_t s_len;
   const int32_t row = rows[blockIdx.x];
   const int32_t keep = keep_lens ? keep_lens[blockIdx.x] : 0;
+  if (threadIdx.x == 0)
+    s_len = row < 0 || row >= o.num_rows || keep < 0
+                ? -1
+                : __hip_atomic_load(&o.seq_lens[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const int32_t n = s_len;
   int32_t bad = 0, gone = 0;
-  if (row < 0 || row >= o.num_rows || keep < 0) {
+  if (n < 0 || n > o.bt_stride * o.page_size) {
     bad = threadIdx.x == 0;
-  } else {
-    const int32_t n = __hip_atomic_load(&o.seq_lens[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (n < 0 || n > o.bt_stride * o.page_size) {
-      bad = threadIdx.x == 0;
-    } else if (keep < n) {
-      int32_t* tab = o.block_tables + (int64_t)row * o.bt_stride;
-      const int32_t held = pages_for(n, o.page_size);
-      for (int32_t j = pages_for(keep, o.page_size) + threadIdx.x; j < held; j += kThreads) {
-        const int32_t e = atomicExch(&tab[j], -1);
-        if (e == -1) continue;                                       // given back already
-        if (e < 0 || e >= o.num_pages) {
-          ++bad;
-        } else if (atomicSub(&o.ref_counts[e], 1) <= 0) {
-          atomicAdd(&o.ref_counts[e], 1);
-          ++bad;
-        } else {
-          ++gone;
-        }
+  } else if (keep < n) {
+    int32_t* tab = o.block_tables + (int64_t)row * o.bt_stride;
+    const int32_t held = pages_for(n, o.page_size);
+    for (int32_t j = pages_for(keep, o.page_size) + threadIdx.x; j < held; j += kThreads) {
+      const int32_t e = atomicExch(&tab[j], -1);
+      if (e == -1) continue;                                         // given back already
+      if (e < 0 || e >= o.num_pages) {
+        ++bad;
+      } else if (atomicSub(&o.ref_counts[e], 1) <= 0) {
+        atomicAdd(&o.ref_counts[e], 1);
+        ++bad;
+      } else {
+        ++gone;
       }
-      __syncthreads();                                               // every thread has its length
-      if (threadIdx.x == 0) atomicMin(&o.seq_lens[row], keep);
     }
+    if (threadIdx.x == 0) atomicMin(&o.seq_lens[row], keep);
   }
   if (gone) atomicAdd(&result[2], gone);
   if (bad) {

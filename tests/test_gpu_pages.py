@@ -152,6 +152,23 @@ def test_bad_rows(tk, call):
     d.call(*call)
 
 
+def test_rows_given_back_several_times_at_once(tk):
+    """Rows of many more pages than a workgroup has threads, named over and over in one call with different lengths to
+    keep: each ends at the smallest, and every page comes back once."""
+    say("[pages] rows named many times")
+    rng = np.random.default_rng(11)
+    rows, stride, P, pages = 5, 1500, 4, 9000
+    tables = rng.permutation(pages)[:rows * stride].reshape(rows, stride)
+    s = Pages([0] * pages, tables, [6000, 5999, 1027, 0, 4500], P)
+    d = Device(tk, s)
+    d.call("count")
+    for most in (6001, 3000, 40):
+        named = rng.integers(0, rows, 200)
+        d.call("free", named, rng.integers(0, most, 200))
+    d.call("free", [0, 1, 2, 3, 4] * 9)
+    assert not any(s.refs)
+
+
 def test_bad_entries(tk):
     """Entries that are no page are carried along or skipped, counted, and never followed."""
     say("[pages] hostile entries")
