@@ -360,7 +360,9 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
     there1 = __ballot(off >= 0);
     if (begin + kTile < count) fetch(1, off);
   }
-  if (begin < count) settle(0, there, !open(begin, wg_first, wg_last), begin + kTile < count);
+  // Whether not all rows of the workgroup see the whole tile: then its values were looked over, for the rows of every wave.
+  bool watch = !open(begin, wg_first, wg_last);
+  if (begin < count) settle(0, there, watch, begin + kTile < count);
   if constexpr (kF8) {
     if (begin + kTile < count) {
       off = locate(begin + kTile, entry);
@@ -512,7 +514,9 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
         if (u == 0 && s + 1 < 4) p[(s + 1) & 1] = weigh(s + 1);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (!clear) {
+      // `watch` alone would do (a wave that is not clear has none but looked-over tiles, or a word that says so), but the
+      // branch that such a wave takes anyway keeps registers free: 8192 tokens 1196 us and 1218, windows 161 and 175.
+      if (!clear || watch) {
         int special = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) special |= s_special[buf][w];
@@ -538,8 +542,8 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
         }
       }
     }
-    if (first + kTile < count)
-      settle(next, there1, !open(first + kTile, wg_first, wg_last), first + 2 * kTile < count);
+    watch = !open(first + kTile, wg_first, wg_last);
+    if (first + kTile < count) settle(next, there1, watch, first + 2 * kTile < count);
     there = there1;
     if constexpr (kBuffers == 3) there1 = there2;
     if constexpr (kF8) {
