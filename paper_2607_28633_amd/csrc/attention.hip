@@ -169,8 +169,11 @@ topkv_status_t describe(const topkv_view_t* v, const topkv_attention_t* t, int32
   a->group = t->num_heads / t->kv_heads;
   a->head_dim = p.head_dim;
   a->value_dim = t->value_dim;
-  a->window = t->window;
-  a->sinks = t->window > 0 ? t->sinks : 0;
+  // A window as wide as the table hides nothing.  Narrower ones, and as many first tokens, leave every difference of a
+  // position and either within 32 bits (a row may stand up to 2^30 before the request's first token).
+  const int32_t cap = v->bt_stride * p.page_size;
+  a->window = t->window < cap ? t->window : 0;
+  a->sinks = a->window == 0 ? 0 : t->sinks < cap ? t->sinks : cap;
   a->scale = scale;
   a->v_scale = t->v_scale;
   a->dtype = t->dtype;
