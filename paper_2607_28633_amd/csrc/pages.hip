@@ -141,6 +141,22 @@ __device__ void plan_rows(const topkv_page_owner_t& o, int32_t num, const int32_
   }
   __threadfence();
   __syncthreads();
+  // The last naming of a row is the good one.  Which store came last is chance: where a row has another's mark the
+  // highest number is found, so that the count of bad rows does not depend on it.
+  bool other = false;
+  for (int32_t i = threadIdx.x; i < num; i += kThreads) {
+    const int32_t row = rows[i];
+    if (row >= 0 && row < o.num_rows)
+      other |= __hip_atomic_load(&w.mark[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i;
+  }
+  if (__syncthreads_or(other)) {
+    for (int32_t i = threadIdx.x; i < num; i += kThreads) {
+      const int32_t row = rows[i];
+      if (row >= 0 && row < o.num_rows) atomicMax(&w.mark[row], i);
+    }
+    __threadfence();
+    __syncthreads();
+  }
   const int32_t per = (num + kThreads - 1) / kThreads;
   const int32_t lo = threadIdx.x * per, hi = lo + per < num ? lo + per : num;
   int64_t want = 0;

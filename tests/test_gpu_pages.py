@@ -152,6 +152,24 @@ def test_bad_rows(tk, call):
     d.call(*call)
 
 
+@pytest.mark.parametrize("seed", range(4))
+def test_bad_rows_are_counted_alike(tk, seed):
+    """Rows named many times, some of their namings bad in themselves too: which of them counts as the good one does not
+    depend on the order of the GPU's stores."""
+    say(f"[pages] one row many times, seed {seed}")
+    rng = np.random.default_rng(seed)
+    rows, P = 700, 4
+    s = Pages([0] * 900, np.full((rows, 3), -1), [0] * rows, P)
+    s.count()
+    assert s.grow([0, 1, 2], [12, 5, 3])[0] == OK
+    d = Device(tk, s)
+    some = rng.choice([3, 5, 699], 640)
+    assert d.call("fork", rng.choice([0, 1, 2, 700, -1], 640), some)[0] == BOUNDS
+    assert d.call("fork", [0] * 639 + [99999], some)[0] == BOUNDS
+    assert d.call("grow", some, rng.choice([0, 4, 12, 13, -2], 640))[0] == BOUNDS
+    assert d.call("grow", [5, 3], [9, 2])[0] == OK
+
+
 def test_rows_given_back_several_times_at_once(tk):
     """Rows of many more pages than a workgroup has threads, named over and over in one call with different lengths to
     keep: each ends at the smallest, and every page comes back once."""
