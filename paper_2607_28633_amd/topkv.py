@@ -224,6 +224,13 @@ def _table_ptr(t) -> int:
     return _ptr(t)
 
 
+def _ints(t, least) -> int:
+    """Address of an int32 tensor that holds `least` words or more (or an address, taken as it is)."""
+    if isinstance(t, torch.Tensor) and t.numel() < least:
+        raise ValueError(f"expected an int32 tensor of at least {least} words, got {t.numel()}")
+    return _table_ptr(t)
+
+
 # The current stream's handle without the Stream object around it (small calls are host-bound: one
 # 100-token layer 9.6 us a call with it, 6.5 us with this and the shorter checks); absent on builds without a GPU.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -912,7 +919,7 @@ def topkv_attention_workspace_bytes(cache: topkv_view_t, attn: topkv_attention_t
 def prepare_attention_decode(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q, out, workspace=None,
                              lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
     wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
-    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)),
+    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_ints(seq_lens, int(num_reqs))),
             *_query_ptrs(cache, attn, q, out, int(num_reqs)), _P(_lse_ptr(lse, int(num_reqs), attn.num_heads)),
             _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
     return PreparedCall("topkv_attention_decode", args, (cache, attn))
@@ -921,8 +928,8 @@ def prepare_attention_decode(cache: topkv_view_t, attn: topkv_attention_t, num_r
 def prepare_attention_prompt(cache: topkv_view_t, attn: topkv_attention_t, num_reqs, seq_lens, q_starts, total_q, q, out,
                              workspace=None, lse=None, workspace_bytes=None, stream=None) -> PreparedCall:
     wsb = 0 if workspace is None else _nbytes(workspace, workspace_bytes)
-    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_table_ptr(seq_lens)),
-            _P(_table_ptr(q_starts)), _I32(int(total_q)), *_query_ptrs(cache, attn, q, out, int(total_q)),
+    args = (ctypes.byref(cache), ctypes.byref(attn), _I32(int(num_reqs)), _P(_ints(seq_lens, int(num_reqs))),
+            _P(_ints(q_starts, int(num_reqs) + 1)), _I32(int(total_q)), *_query_ptrs(cache, attn, q, out, int(total_q)),
             _P(_lse_ptr(lse, int(total_q), attn.num_heads)), _P(_ptr(workspace)), _I64(wsb), _P(_stream(stream)))
     return PreparedCall("topkv_attention_prompt", args, (cache, attn))
 
@@ -950,8 +957,9 @@ def page_owner(ref_counts, block_tables, seq_lens, *, page_size, num_pages=None,
         num_pages = ref_counts.numel()
     if num_rows is None or bt_stride is None:
         num_rows, bt_stride = block_tables.shape
-    return topkv_page_owner_t(_table_ptr(ref_counts), _table_ptr(block_tables), _table_ptr(seq_lens), int(num_pages),
-                              int(page_size), int(num_rows), int(bt_stride), 0)
+    num_pages, num_rows, bt_stride = int(num_pages), int(num_rows), int(bt_stride)
+    return topkv_page_owner_t(_ints(ref_counts, num_pages), _ints(block_tables, num_rows * bt_stride),
+                              _ints(seq_lens, num_rows), num_pages, int(page_size), num_rows, bt_stride, 0)
 
 
 def _pairs(t, given):
@@ -959,7 +967,7 @@ def _pairs(t, given):
         if not isinstance(t, torch.Tensor):
             raise ValueError("the number of pairs is required when passing a raw address")
         given = t.numel() // 2
-    return _P(_table_ptr(t)), _I32(int(given))
+    return _P(_ints(t, 2 * int(given))), _I32(int(given))
 
 
 def topkv_pages_workspace_bytes(owner: topkv_page_owner_t) -> int:
@@ -972,36 +980,36 @@ def topkv_pages_workspace_bytes(owner: topkv_page_owner_t) -> int:
 def topkv_pages_count(owner: topkv_page_owner_t, result, stream=None) -> None:
     """ref_counts from the tables; result (device int32[4], for every call
     here): [status, pairs, pages, bad rows or entries]."""
-    _check(_lib.topkv_pages_count(ctypes.byref(owner), _table_ptr(result), _stream(stream)))
+    _check(_lib.topkv_pages_count(ctypes.byref(owner), _ints(result, 4), _stream(stream)))
 
 
 def topkv_pages_free(owner: topkv_page_owner_t, num, rows, result, keep_lens=None, stream=None) -> None:
     """Rows give back the pages past their first keep_lens[i] tokens (None: all)."""
-    _check(_lib.topkv_pages_free(ctypes.byref(owner), int(num), _table_ptr(rows), _table_ptr(keep_lens),
-                                 _table_ptr(result), _stream(stream)))
+    _check(_lib.topkv_pages_free(ctypes.byref(owner), int(num), _ints(rows, num), _ints(keep_lens, num), _ints(result, 4),
+                                 _stream(stream)))
 
 
 def topkv_pages_fork(owner: topkv_page_owner_t, num, parents, children, pairs, workspace, result, max_pairs=None,
                      workspace_bytes=None, stream=None) -> None:
     """Rows children[i] branch off rows parents[i]."""
-    _check(_lib.topkv_pages_fork(ctypes.byref(owner), int(num), _table_ptr(parents), _table_ptr(children),
+    _check(_lib.topkv_pages_fork(ctypes.byref(owner), int(num), _ints(parents, num), _ints(children, num),
                                  *_pairs(pairs, max_pairs), _ptr(workspace), _nbytes(workspace, workspace_bytes),
-                                 _table_ptr(result), _stream(stream)))
+                                 _ints(result, 4), _stream(stream)))
 
 
 def topkv_pages_grow(owner: topkv_page_owner_t, num, rows, new_lens, pairs, workspace, result, max_pairs=None,
                      workspace_bytes=None, stream=None) -> None:
     """Rows take the pages for new_lens[i] tokens."""
-    _check(_lib.topkv_pages_grow(ctypes.byref(owner), int(num), _table_ptr(rows), _table_ptr(new_lens),
+    _check(_lib.topkv_pages_grow(ctypes.byref(owner), int(num), _ints(rows, num), _ints(new_lens, num),
                                  *_pairs(pairs, max_pairs), _ptr(workspace), _nbytes(workspace, workspace_bytes),
-                                 _table_ptr(result), _stream(stream)))
+                                 _ints(result, 4), _stream(stream)))
 
 
 def topkv_pages_compact(owner: topkv_page_owner_t, pairs, workspace, result, max_pairs=None, workspace_bytes=None,
                         stream=None) -> None:
     """Move the live pages together at the pool's lower end."""
     _check(_lib.topkv_pages_compact(ctypes.byref(owner), *_pairs(pairs, max_pairs), _ptr(workspace),
-                                    _nbytes(workspace, workspace_bytes), _table_ptr(result), _stream(stream)))
+                                    _nbytes(workspace, workspace_bytes), _ints(result, 4), _stream(stream)))
 
 
 def topkv_copy_pages(src, dst, first_layer, num_layers, pairs, max_pairs=None, count=None, stream=None) -> None:
@@ -1009,4 +1017,4 @@ def topkv_copy_pages(src, dst, first_layer, num_layers, pairs, max_pairs=None, c
     count: a device int32 (tensor or address), or None for all pairs."""
     ptr, most = _pairs(pairs, max_pairs)
     _check(_lib.topkv_copy_pages(ctypes.byref(_pool_arg(src)), ctypes.byref(_pool_arg(dst)), int(first_layer),
-                                 int(num_layers), ptr, most, _table_ptr(count), _stream(stream)))
+                                 int(num_layers), ptr, most, _ints(count, 1), _stream(stream)))

@@ -155,3 +155,41 @@ def test_copy_pages_refused(tk):  # noqa: F811
     _expect(tk, UNS, copy, _pool(tk, num_pages=1 << 40, num_layers=1 << 20), good, 0, 1, 0x6000, max_pairs=3)
     copy(good, good, 0, 0, 0, max_pairs=3, stream=0)
     copy(good, good, 0, 2, 0, max_pairs=0, stream=0)
+
+
+def _ints(*shape):
+    import torch
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def test_short_tensors_refused(tk):  # noqa: F811
+    """Index tensors that are shorter than the call reads or writes never reach the library."""
+    view, opt, o = _view(tk, _pool(tk)), _options(tk), _owner(tk)
+    need = tk.topkv_pages_workspace_bytes(o)
+    room = dict(workspace_bytes=1 << 40, stream=0)
+    page = dict(max_pairs=9, workspace_bytes=need, stream=0)
+    calls = [
+        lambda: tk.topkv_attention_decode(view, opt, 3, _ints(2), 0x4000, 0x5000, 0x10000, **room),
+        lambda: tk.topkv_attention_prompt(view, opt, 3, _ints(2), 0x3000, 5, 0x4000, 0x5000, 0x10000, **room),
+        lambda: tk.topkv_attention_prompt(view, opt, 3, 0x3000, _ints(3), 5, 0x4000, 0x5000, 0x10000, **room),
+        lambda: tk.page_owner(_ints(10), 0x2000, 0x3000, page_size=16, num_pages=11, num_rows=2, bt_stride=4),
+        lambda: tk.page_owner(0x1000, _ints(2, 4), 0x3000, page_size=16, num_pages=11, num_rows=2, bt_stride=5),
+        lambda: tk.page_owner(0x1000, 0x2000, _ints(1), page_size=16, num_pages=11, num_rows=2, bt_stride=4),
+        lambda: tk.topkv_pages_count(o, _ints(3), stream=0),
+        lambda: tk.topkv_pages_free(o, 3, _ints(2), 0x9000, stream=0),
+        lambda: tk.topkv_pages_free(o, 3, 0x4000, 0x9000, _ints(2), stream=0),
+        lambda: tk.topkv_pages_free(o, 3, 0x4000, _ints(3), stream=0),
+        lambda: tk.topkv_pages_fork(o, 3, _ints(2), 0x5000, 0x6000, 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_fork(o, 3, 0x4000, _ints(2), 0x6000, 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_fork(o, 3, 0x4000, 0x5000, _ints(8, 2), 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_fork(o, 3, 0x4000, 0x5000, 0x6000, 0x10000, _ints(1), **page),
+        lambda: tk.topkv_pages_grow(o, 3, _ints(2), 0x5000, 0x6000, 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_grow(o, 3, 0x4000, _ints(1), 0x6000, 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_grow(o, 3, 0x4000, 0x5000, 0x6000, 0x10000, _ints(0), **page),
+        lambda: tk.topkv_pages_compact(o, _ints(8, 2), 0x10000, 0x9000, **page),
+        lambda: tk.topkv_pages_compact(o, 0x6000, 0x10000, _ints(3), max_pairs=50, workspace_bytes=need, stream=0),
+        lambda: tk.topkv_copy_pages(_pool(tk), _pool(tk), 0, 1, _ints(2, 2), max_pairs=3, stream=0),
+        lambda: tk.topkv_copy_pages(_pool(tk), _pool(tk), 0, 1, 0x6000, max_pairs=3, count=_ints(0), stream=0)]
+    for call in calls:
+        with pytest.raises(ValueError, match="at least"):
+            call()
