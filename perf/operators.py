@@ -306,12 +306,11 @@ def _own_beams(s):
     topkv = _own_handles(s)
     c, kids = s["case"], s["children"]
     n = kids.shape[0]
-    if "longer" not in s:
-        s["longer"] = (s["lens"][s["parents"].long()] + 1).contiguous()
     topkv.topkv_pages_free(s["owner"], n, kids, s["result"])
     topkv.topkv_pages_fork(s["owner"], n, s["parents"], kids, s["pairs"], s["work"], s["result"])
     topkv.topkv_copy_pages(s["pool"], s["pool"], 0, c["layers"], s["pairs"], n, s["result"][1:])
-    topkv.topkv_pages_grow(s["owner"], n, kids, s["longer"], s["pairs"], s["work"], s["result"])
+    longer = s["lens"][c["rows"]:] + 1                                 # the children's rows come last
+    topkv.topkv_pages_grow(s["owner"], n, kids, longer, s["pairs"], s["work"], s["result"])
     return {"tables": s["tables"], "lens": s["lens"], "refs": s["refs"], "pool": s["pool"]}
 
 
