@@ -625,8 +625,12 @@ topkv_status_t topkv_reblock_layer(const topkv_pool_t* src, int32_t src_layer, c
  *     out = v_scale * sum_V exp(x_j) v_j / sum_V exp(x_j)
  *     lse = ln sum_V exp(x_j)
  * and out = 0, lse = -inf where V is empty (a request of no tokens among
- * them) or every x_j in it is -inf.  What a cache holds outside V never reaches a row's result, NaN and
- * infinities included.  Sums and softmax statistics are 32-bit floats. */
+ * them) or every x_j in it is -inf.  What a cache holds outside V never reaches
+ * a row's result, NaN and infinities included; a NaN or an infinity among the
+ * values of V makes its element of out a NaN or an infinity.
+ * Scores, sums and softmax statistics are 32-bit floats.  Where the matrix
+ * units do the work, exp(x_j) is rounded to q's type (by at most 2^-8 of it in
+ * bf16, 2^-11 in fp16) for its product with v_j, in the upper sum alone. */
 typedef enum topkv_dtype {
   TOPKV_BF16 = 0,
   TOPKV_FP16 = 1,
@@ -778,8 +782,9 @@ topkv_status_t topkv_pages_grow(const topkv_page_owner_t* owner, int32_t num, co
  * pairs (at most num_pages / 2) say what to copy.  Held entries outside the
  * pool and rows of bad length stay as they are and are counted in result[3]
  * (result[0] TOPKV_ERR_BOUNDS; the rest is moved).  ref_counts have to agree
- * with the tables (topkv_pages_count): an entry that names a free page may
- * name another row's page afterwards.
+ * with the tables (topkv_pages_count): an entry that names a free page counts
+ * as bad where that page is U or above, and may name another row's page
+ * afterwards where it is below.
  *   pairs: device int32[max_pairs][2], max_pairs >= num_pages / 2 */
 topkv_status_t topkv_pages_compact(const topkv_page_owner_t* owner, int32_t* pairs, int32_t max_pairs,
                                    void* workspace, int64_t workspace_bytes, int32_t* result,

@@ -1,5 +1,5 @@
 // attention.h - what the attention kernels share (attention.hip: the calls and
-// the general kernel; attention_decode.hip, attention_prompt.hip: the matrix-unit kernels).
+// the general kernel; attention_decode.hip, attention_latent.hip, attention_prompt.hip: the matrix-unit kernels).
 #ifndef TOPKV_ATTENTION_H_
 #define TOPKV_ATTENTION_H_
 

@@ -9,9 +9,11 @@
 // of a workgroup share a tile of 32 keys.  For the scores a wave takes 16 keys,
 // 16 rows and, where there are few rows, a half or a quarter of the elements;
 // the parts meet in LDS, from where the weights come that a wave multiplies with
-// its 64 elements of the values.  Three tiles are in LDS,
-// one in use and two on their way straight from memory, which is what keeps
-// the bytes coming: a CU holds one workgroup.
+// its 64 elements of the values.  Three tiles are in LDS, straight from memory:
+// one in use, and two asked for ahead, since a CU holds one workgroup.  Of
+// these two only the later is under way while a tile is multiplied: the compiler,
+// which does not see loads to LDS, waits for all loads where it uses the table
+// entry that it asked for before them, once a tile.
 #include <type_traits>
 
 #include "attention_internal.h"
@@ -191,7 +193,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_attention_latent_kernel(Args a
   for (int32_t first = begin; first < end; first += kTile) {
     const int next = buf + 1 < kBuffers ? buf + 1 : 0, last = next + 1 < kBuffers ? next + 1 : 0;
     if constexpr (!kF8) {
-      // this wave's part of the tile has landed when no more than the next tile's loads (4 at least) are under way
+      // this wave's part of the tile has landed when no more than the next tile's loads (4 at least) are under way; those
+      // are waited for below, where the compiler uses `entry`
       // (narrower rows: some of a tile's loads may have no lane to them and are never issued)
       if (first + kTile < end && chunks == NC) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
       else wait_loads();

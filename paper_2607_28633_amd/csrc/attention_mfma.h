@@ -1,12 +1,21 @@
 // attention_mfma.h - types, matrix instructions and cross-lane steps of the
 // matrix-unit attention kernels.
 //
-// Both kernels compute the transposed products: scores^T = K Q^T and
+// All of them compute the transposed products: scores^T = K Q^T and
 // out^T += V^T P^T, so that a query row is a column of every accumulator and
 // its maximum, sum and scale live in the lanes that hold the column.  The
 // scores' accumulator layout (4 consecutive keys per lane) is also a valid
 // layout of the second product's operand once both sides number the keys the
-// same way, so the weights never leave their registers.
+// same way, so that decode's and the prompts' weights never leave their
+// registers; a latent cache's scores or weights pass through LDS, where waves
+// share a row.
+//
+// The second product takes weights and values in one 16-bit type: a weight is
+// rounded once, by at most half a step of that type, its sum (the divisor) is
+// made of the weights before.  Against 64 bits the results are off 1.1 to 1.4
+// times as far as those of a computation in 32 bits rounded once (8192 tokens:
+// 0.0021 and 0.0016 relative, bf16's half step being 0.0039); two products, of
+// a weight's upper and lower half, would take the second one's time twice.
 #ifndef TOPKV_ATTENTION_MFMA_H_
 #define TOPKV_ATTENTION_MFMA_H_
 

@@ -8,8 +8,9 @@
 // 256 * head_dim bytes of LDS: a wave's keys and values come out of LDS at the
 // rate at which the matrix units take them, and the softmax between the two
 // products is what has to hide behind the other wave of the SIMD.  While a
-// tile is multiplied the next one or two are on their way to LDS (an 8-bit
-// cache through registers): one barrier a tile.
+// tile is multiplied another is on its way to LDS (an 8-bit cache through
+// registers): the next, or with eight waves the one after it, so that a tile
+// has landed a tile before it is used.  One barrier a tile.
 //
 // Many row tiles keep the GPU busy by themselves, the longest started first.
 // Few of them (a short chunk behind a long cache, one KV head) are cut along
@@ -264,7 +265,8 @@ __global__ __launch_bounds__(64 * kWaves, resident(KD) / 256) void kv_attention_
   float slack = kSlack;
 
   // Lane k of every wave looks after key k of the tile: its table entry is asked for before the tile's rows of the
-  // step before, its row's offset is handed to the lanes that load the row.
+  // step before, its row's offset is handed to the lanes that load the row.  Where rows go straight to LDS the compiler
+  // does not see their loads, and waits for them too where it uses the entry.
   const auto ask = [&](int32_t first) -> int32_t {
     const int32_t v = first + lane;
     return v < span.count ? table[page_of(a, (uint32_t)key_position(span, v))] : -1;
@@ -680,8 +682,8 @@ int64_t most_keys(const Args& a) {
   return a.window > 0 && (int64_t)a.window + a.sinks < seen ? (int64_t)a.window + a.sinks : seen;
 }
 
-// Eight waves on one tile halve the loads of a row and have two tiles on their way, four waves twice over a CU start
-// and end more easily.  8192 tokens, heads of 128: 8 waves 1204 us, 4 1278; windows of 128, heads of 64, in
+// Eight waves on one tile halve the loads of a row and ask for it a tile earlier, four waves twice over a CU start and
+// end more easily.  8192 tokens, heads of 128: 8 waves 1204 us, 4 1278; windows of 128, heads of 64, in
 // an earlier form: 250 and 180.  Heads of 256 have no registers for more than one wave a SIMD.
 int waves_for(const Args& a) {
   return a.head_dim > 64 && a.head_dim <= 128 && most_keys(a) >= 1024 &&
