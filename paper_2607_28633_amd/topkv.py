@@ -952,7 +952,8 @@ def topkv_attention_prompt(cache: topkv_view_t, attn: topkv_attention_t, num_req
 def page_owner(ref_counts, block_tables, seq_lens, *, page_size, num_pages=None, num_rows=None,
                bt_stride=None) -> topkv_page_owner_t:
     """Descriptor of who holds which page: int32 tensors ref_counts [pages],
-    block_tables [rows][stride] and seq_lens [rows] (or addresses with the sizes given)."""
+    block_tables [rows][stride] and seq_lens [rows] (or addresses with the sizes given).
+    It holds addresses: the tensors have to outlive it."""
     if num_pages is None:
         num_pages = ref_counts.numel()
     if num_rows is None or bt_stride is None:

@@ -82,3 +82,19 @@ def test_prompt_few_tokens_of_many_requests(tk, kw, reqs, most):  # noqa: F811
     c.call(tk)
     ends = {int(c.starts[r]) + d for r in some for d in (0, most // 2, most - 1)}
     c.check(c.exact(only=ends | set(rng.integers(0, c.total, 50).tolist())))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(kv=1, group=8), dict(dim=25, kv=1), dict(dim=64, kv_type=F8)])
+@pytest.mark.parametrize("starts", [[0, 100, 50, 120], [120, 0, 120, 0], [7, -3, 2**31 - 1, 5], [-2**31, 2**31 - 1, -2**31, 2**31 - 1]])
+def test_starts_that_do_not_ascend(tk, kw, starts):  # noqa: F811
+    """Nothing outside q's rows is written, and a good call afterwards is right: the workspace keeps nothing."""
+    say(f"[attention] q_starts {starts} {kw}")
+    c = Case(83, [900, 30, 70], [60, 20, 40], **kw).device(tk)
+    good = c.starts_d.clone()
+    c.starts_d.copy_(torch.tensor(starts, dtype=torch.int64).to(torch.int32).cuda())
+    c.call(tk)
+    torch.cuda.synchronize()
+    assert (c.out_full[c.total:] == 77).all() and (c.lse_d[c.total:] == 77).all()
+    c.starts_d.copy_(good)
+    c.call(tk)
+    c.check()

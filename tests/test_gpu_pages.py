@@ -201,6 +201,20 @@ def test_bad_entries(tk):
     d.call("free", [0, 1, 2, 3])
 
 
+def test_compact_with_entries_of_free_pages(tk):
+    """Counts that do not agree with the tables: an entry of a free page at U or above is counted and stays, one below U
+    stays too, and nothing else goes wrong."""
+    say("[pages] compact, entries of free pages")
+    refs, tables = to_dev(np.array([1, 0, 1, 0, 0, 0], np.int32)), to_dev(np.array([[0, 2], [4, 1]], np.int32))
+    lens = to_dev(np.array([8, 7], np.int32))                     # an owner holds addresses, not the tensors
+    owner = tk.page_owner(refs, tables, lens, page_size=4)
+    work = torch.full((tk.topkv_pages_workspace_bytes(owner),), 0, dtype=torch.uint8, device="cuda")
+    pairs, result = torch.zeros((3, 2), dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    tk.topkv_pages_compact(owner, pairs, work, result)
+    assert result.tolist() == [BOUNDS, 1, 2, 1] and pairs[0].tolist() == [2, 1]
+    assert refs.tolist() == [1, 1, 0, 0, 0, 0] and tables.tolist() == [[0, 1], [4, 1]]
+
+
 def test_empty_calls(tk):
     s, _ = make(3, 4, 3, 20, 4)
     d = Device(tk, s)
